@@ -293,6 +293,90 @@ int mslt_debug_attention(void* hip_stream, int precision, int batch, int seq, in
                          const int32_t* attn_mask, float mask_bias, float dropout, uint64_t seed, void* ctx, float* ctx_f32,
                          float* lse, const void* dctx, float* delta, void* dqkv);
 
+/* ---- operators between a layer's QKV projection and its output projection ----------------------------------------
+ * For models whose layers differ from BERT's in how queries and keys are prepared and how they attend; as
+ * mslt_debug_attention they take DEVICE operands, enqueue on hip_stream (hipStream_t as void*, null = default stream) of
+ * the current device, return MSLT_ERR_ARG before anything is enqueued, never block, allocate nothing and may be captured
+ * into a graph.  precision 0: fp32 operands, 1: bf16.  Operands must not overlap unless said otherwise.  Two calls that
+ * may run at the same time need a workspace each. */
+
+/* Heads in DEVICE memory: element i of head h of token s of sequence b lies at data + b*batch_stride + s*row_stride +
+ * h*head_stride + i (strides in elements, not negative).  Parts of a packed projection, [batch, seq, heads, width] and
+ * [batch, heads, seq, width] all are such.  What a call writes must not overlap itself. */
+typedef struct {
+  void* data;
+  long long batch_stride, row_stride, head_stride;
+} mslt_heads;
+
+/* Rotary positions: pair i < rotary_width/2 of a head turns by position * f_i, f_i = theta^(-2i/rotary_width), scaled:
+ * scaling 0 no; 1 f_i/factor; 2 by how often the pair turns within original_length positions, w = original_length*f_i/2pi:
+ * f_i * (t + (1-t)/factor), t = (w - low_turns)/(high_turns - low_turns) held to 0..1.  Pair i is elements (i, i +
+ * rotary_width/2), or (2i, 2i+1) when interleaved; elements from rotary_width on stay as they are.  The rotated elements
+ * are multiplied by magnitude.  Angles are exact to 2^-32 of a turn at any position. */
+typedef struct {
+  int rotary_width;   /* even, 0 to the head width */
+  int interleaved;
+  int scaling;
+  double theta;       /* > 1 */
+  double factor;      /* > 0; scaling 1 and 2 */
+  double original_length, low_turns, high_turns; /* scaling 2: > 0, low < high */
+  float magnitude;
+} mslt_rotary_form;
+
+/* Turns every head of q and, unless k is null, of k (k_heads of them); inverse != 0: by the negative angles, which is also
+ * the gradient.  positions: [batch, seq], or null for 0 .. seq-1.  width at most 256.  q_out may be q itself (same
+ * strides), k_out k. */
+int mslt_rotary(void* hip_stream, int precision, int batch, int seq, int q_heads, int k_heads, int width, const mslt_heads* q,
+                const mslt_heads* k, const int32_t* positions, const mslt_rotary_form* form, int inverse,
+                const mslt_heads* q_out, const mslt_heads* k_out);
+
+/* The same rotation of x * gain / sqrt(mean(x^2) + eps), the mean over each head.  gain_q, gain_k: fp32 [width], or
+ * [heads, width] with gain_per_head != 0. */
+int mslt_head_norm_rotary(void* hip_stream, int precision, int batch, int seq, int q_heads, int k_heads, int width,
+                          const mslt_heads* q, const mslt_heads* k, const float* gain_q, const float* gain_k, int gain_per_head,
+                          float eps, const int32_t* positions, const mslt_rotary_form* form, const mslt_heads* q_out,
+                          const mslt_heads* k_out);
+
+/* Its gradients: q, k as the forward got them, grad_q, grad_k those of its outputs; dq, dk (may be grad_q, grad_k
+ * themselves) of its inputs; dgain_q, dgain_k fp32 as the gains, sums over all tokens (and over the heads of a shared
+ * gain) in a fixed order.  workspace: DEVICE scratch of the bytes that mslt_head_norm_workspace reports. */
+int mslt_head_norm_rotary_backward(void* hip_stream, int precision, int batch, int seq, int q_heads, int k_heads, int width,
+                                   const mslt_heads* q, const mslt_heads* k, const float* gain_q, const float* gain_k,
+                                   int gain_per_head, float eps, const int32_t* positions, const mslt_rotary_form* form,
+                                   const mslt_heads* grad_q, const mslt_heads* grad_k, const mslt_heads* dq, const mslt_heads* dk,
+                                   float* dgain_q, float* dgain_k, void* workspace, size_t workspace_bytes);
+int mslt_head_norm_workspace(int batch, int seq, int q_heads, int k_heads, int width, size_t* bytes);
+
+/* How queries and keys attend.  Query i of n stands at position keys - n + i.  Score: scale * q.k, then cap * tanh(score /
+ * cap) when cap > 0, then - slopes[head] * |distance of the positions| when slopes is given.  A query sees a key of its own
+ * document only (the same entry of documents, not negative), and with causal != 0 only keys at its position or before, or
+ * among the first prefix[b] of its sequence.  A query that sees no key gets zeros, a log-sum-exp of -infinity, and no
+ * gradient.  Rows of a negative document (padding) may hold anything, NaN included: none of it is used, their outputs and
+ * gradients are zeros.  All other rows must be finite, and scores within 1e30. */
+typedef struct {
+  float scale;              /* finite, > 0 */
+  float cap;                /* 0: none */
+  int causal;
+  const int32_t* documents; /* DEVICE [batch, keys], or null: one document */
+  const int32_t* prefix;    /* DEVICE [batch], or null; only with causal */
+  const float* slopes;      /* DEVICE [heads], or null */
+} mslt_attention_form;
+
+/* out = softmax(scores) v.  q, out: queries x heads; k, v: keys x kv_heads, head h reads kv head h / (heads / kv_heads).
+ * 1 <= queries <= keys; heads a multiple of kv_heads; width at most 128; data, strides and width multiples of 16 bytes.
+ * lse: fp32 [batch, heads, queries], natural log-sum-exp of the scores.  workspace: DEVICE scratch, 16-byte aligned, of
+ * the bytes that mslt_attention_workspace reports for the direction. */
+int mslt_attention(void* hip_stream, int precision, int batch, int queries, int keys, int heads, int kv_heads, int width,
+                   const mslt_heads* q, const mslt_heads* k, const mslt_heads* v, const mslt_attention_form* form,
+                   const mslt_heads* out, float* lse, void* workspace, size_t workspace_bytes);
+/* Gradients of q, k and v from that of out, given what the forward left. */
+int mslt_attention_backward(void* hip_stream, int precision, int batch, int queries, int keys, int heads, int kv_heads, int width,
+                            const mslt_heads* q, const mslt_heads* k, const mslt_heads* v, const mslt_heads* out, const float* lse,
+                            const mslt_heads* grad_out, const mslt_attention_form* form, const mslt_heads* dq, const mslt_heads* dk,
+                            const mslt_heads* dv, void* workspace, size_t workspace_bytes);
+int mslt_attention_workspace(int precision, int batch, int queries, int keys, int heads, int kv_heads, int width, int backward,
+                             size_t* bytes);
+
 /* Waits until all work enqueued on the model's stream has finished. */
 int mslt_sync(const mslt_model* m);
 

@@ -21,6 +21,8 @@ EXPORTS = [
     "mslt_debug_prefix_output", "mslt_grow", "mslt_sync", "mslt_destroy", "mslt_last_error",
     "mslt_profile_enable", "mslt_profile_read", "mslt_debug_gemm",
     "mslt_debug_attention", "mslt_debug_plan_gemm", "mslt_debug_plan_chains", "mslt_debug_gemm_epilogue",
+    "mslt_rotary", "mslt_head_norm_rotary", "mslt_head_norm_rotary_backward", "mslt_head_norm_workspace",
+    "mslt_attention", "mslt_attention_backward", "mslt_attention_workspace",
 ]
 
 MSLT_OK, MSLT_ERR_ARG, MSLT_ERR_STATE, MSLT_ERR_DATA, MSLT_ERR_HIP, MSLT_ERR_NONFINITE = 0, -1, -2, -3, -4, -5
@@ -58,6 +60,20 @@ class TensorDesc(C.Structure):
 class DebugEpilogue(C.Structure):
     _fields_ = [("bias", C.c_void_p), ("act", C.c_int), ("gelu_grad", C.c_void_p), ("aux", C.c_void_p), ("aux_f32", C.c_int),
                 ("dropout", C.c_float), ("seed", C.c_uint64), ("accumulate", C.c_int)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_longlong), ("row_stride", C.c_longlong), ("head_stride", C.c_longlong)]
+
+
+class RotaryForm(C.Structure):
+    _fields_ = [("rotary_width", C.c_int), ("interleaved", C.c_int), ("scaling", C.c_int), ("theta", C.c_double), ("factor", C.c_double),
+                ("original_length", C.c_double), ("low_turns", C.c_double), ("high_turns", C.c_double), ("magnitude", C.c_float)]
+
+
+class AttentionForm(C.Structure):
+    _fields_ = [("scale", C.c_float), ("cap", C.c_float), ("causal", C.c_int), ("documents", C.c_void_p), ("prefix", C.c_void_p),
+                ("slopes", C.c_void_p)]
 
 
 class ProfileEntry(C.Structure):
@@ -101,6 +117,16 @@ def load_library():
     lib.mslt_debug_plan_gemm.argtypes = [C.c_int] * 7 + [P(C.c_int)] * 4
     lib.mslt_debug_plan_chains.argtypes = [P(Config), C.c_int, C.c_int, C.c_int, P(C.c_int)]
     lib.mslt_debug_attention.argtypes = [vp] + [C.c_int] * 5 + [vp, vp, C.c_float, C.c_float, C.c_uint64] + [vp] * 6
+    sizes6, H = [C.c_int] * 6, P(Heads)      # precision and the five sizes that q and k share
+    norm = [vp] + sizes6 + [H, H, vp, vp, C.c_int, C.c_float, vp, P(RotaryForm)]
+    lib.mslt_rotary.argtypes = [vp] + sizes6 + [H, H, vp, P(RotaryForm), C.c_int, H, H]
+    lib.mslt_head_norm_rotary.argtypes = norm + [H, H]
+    lib.mslt_head_norm_rotary_backward.argtypes = norm + [H, H, H, H, vp, vp, vp, sz]
+    lib.mslt_head_norm_workspace.argtypes = [C.c_int] * 5 + [P(sz)]
+    att = [vp] + [C.c_int] * 7 + [H, H, H]
+    lib.mslt_attention.argtypes = att + [P(AttentionForm), H, vp, vp, sz]
+    lib.mslt_attention_backward.argtypes = att + [H, vp, H, P(AttentionForm), H, H, H, vp, sz]
+    lib.mslt_attention_workspace.argtypes = [C.c_int] * 8 + [P(sz)]
     lib.mslt_destroy.argtypes = [vp]
     lib.mslt_last_error.argtypes = []
     lib.mslt_last_error.restype = C.c_char_p
@@ -193,6 +219,229 @@ def mslt_debug_attention(qkv, attn_mask, n_heads, head_width, mask_bias=-10000.0
                                                ptr(out.get("dqkv"))))
     out["delta"] = delta      # (kept alive with the rest while the kernels are queued)
     return out
+
+
+# -- operators between a layer's QKV projection and its output projection
+def _refusal(message):
+    return MsltError(MSLT_ERR_ARG, message)
+
+
+class _Place:
+    """Where a call runs: the device of its first tensor, and `stream` or that device's current one.  Inside the `with`,
+    tensors come from that stream's memory; tensors of another stream are marked as used on it."""
+
+    def __init__(self, name, stream, tensors):
+        import torch
+        if not tensors[0].is_cuda:
+            raise _refusal(f"{name}: tensors must be on a GPU")
+        index = tensors[0].device.index
+        for t in tensors:
+            if t is not None and t.device.index != index:
+                raise _refusal(f"{name}: tensors on different devices")
+        current = torch.cuda.current_stream(index)
+        self.stream, self.guard = current, None
+        if stream is not None and stream != current:
+            if stream.device.index != index:
+                raise _refusal(f"{name}: the stream is another device's")
+            self.stream = stream
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+        if self.stream is not current or torch.cuda.current_device() != index:
+            self.guard = torch.cuda.stream(self.stream)      # (switches the device with it)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return C.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _precision(name, t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return 1
+    if t.dtype is torch.float32:
+        return 0
+    raise _refusal(f"{name}: bf16 or fp32 tensors, not {t.dtype}")
+
+
+def _heads(name, what, t, like=None, shape=None):
+    """A 4-D tensor [batch, rows, heads, width] as the C struct; like: must have its type."""
+    if t.dim() != 4 or (shape is not None and t.shape != shape):
+        raise _refusal(f"{name}: {what} must be [batch, rows, heads, width]" + (f" {tuple(shape)}" if shape is not None else "") +
+                         f", not {tuple(t.shape)}")
+    if like is not None and t.dtype is not like.dtype:
+        raise _refusal(f"{name}: {what} is {t.dtype}, not {like.dtype}")
+    sb, sr, sh, se = t.stride()
+    if se != 1 and t.shape[3] > 1:
+        raise _refusal(f"{name}: the elements of a head of {what} must be next to each other")
+    return Heads(t.data_ptr(), sb, sr, sh)
+
+
+def _flat(name, what, t, dtype, *shapes):
+    """Address of a contiguous tensor of one of the given shapes; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_contiguous() or all(t.shape != s for s in shapes):
+        raise _refusal(f"{name}: {what} must be contiguous {dtype} {' or '.join(str(tuple(s)) for s in shapes)}, "
+                         f"not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+_SCALINGS = {"none": 0, "linear": 1, "ramp": 2}
+
+
+def rotary_form(rotary_width, interleaved=False, theta=10000.0, scaling="none", factor=1.0, original_length=0, low_turns=1.0,
+                high_turns=32.0, magnitude=1.0) -> RotaryForm:
+    """How positions turn the heads, see mslt_rotary_form in the header; scaling: none, linear or ramp."""
+    if scaling not in _SCALINGS:
+        raise _refusal(f"rotary_form: scaling must be one of {', '.join(_SCALINGS)}, not {scaling!r}")
+    return RotaryForm(rotary_width, int(interleaved), _SCALINGS[scaling], theta, factor, original_length, low_turns, high_turns, magnitude)
+
+
+def _rotary_sizes(name, q, k):
+    B, S, hq, w = q.shape if q.dim() == 4 else (0, 0, 0, 0)
+    if k is not None and (k.dim() != 4 or (k.shape[0], k.shape[1], k.shape[3]) != (B, S, w)):
+        raise _refusal(f"{name}: q {tuple(q.shape)} and k {tuple(k.shape)} differ in more than their heads")
+    return B, S, hq, 0 if k is None else k.shape[2], w
+
+
+def _results(name, what, given, inputs):
+    """The tensors results go to: the given ones, or new contiguous ones."""
+    import torch
+    given = given if given is not None else (None,) * len(inputs)
+    if len(given) != len(inputs):
+        raise _refusal(f"{name}: {what} must hold {len(inputs)} tensors")
+    return [x if o is None and x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) if o is None else o
+            for o, x in zip(given, inputs)]
+
+
+def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None, stream=None):
+    """Rotary positions of q [batch, seq, heads, width] and k (its own number of heads, or None), any strides with contiguous
+    elements.  positions: int32 [batch, seq], default 0 .. seq-1.  inverse: by the negative angles, the gradient.  out: tensors
+    for the results, q and k themselves allowed.  Returns them.  Enqueues only."""
+    import torch
+    name = "mslt_rotary"
+    B, S, hq, hk, w = _rotary_sizes(name, q, k)
+    with _Place(name, stream, [q, k, positions] + list(out or ())) as st:
+        oq, ok = _results(name, "out", out, (q, k))
+        hq_in, hq_out = _heads(name, "q", q), _heads(name, "out", oq, q, q.shape)
+        hk_in = hk_out = None
+        if k is not None:
+            hk_in, hk_out = C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "out", ok, q, k.shape))
+        _check(load_library().mslt_rotary(st, _precision(name, q), B, S, hq, hk, w, C.byref(hq_in), hk_in,
+                                          _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form), int(inverse),
+                                          C.byref(hq_out), hk_out))
+    return oq, ok
+
+
+def _gains(name, gain_q, gain_k, hq, hk, w):
+    import torch
+    per_head = int(gain_q.dim() == 2)
+    shapes = ((hq, w), (hk, w)) if per_head else ((w,), (w,))
+    return (_flat(name, "gain_q", gain_q, torch.float32, shapes[0]), _flat(name, "gain_k", gain_k, torch.float32, shapes[1]), per_head)
+
+
+def mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form: RotaryForm, positions=None, out=None, stream=None):
+    """mslt_rotary of x * gain / sqrt(mean(x^2) + eps) over each head.  gains: fp32 [width], or [heads, width] each.  Returns
+    the two results.  Enqueues only."""
+    import torch
+    name = "mslt_head_norm_rotary"
+    B, S, hq, hk, w = _rotary_sizes(name, q, k)
+    with _Place(name, stream, [q, k, gain_q, gain_k, positions] + list(out or ())) as st:
+        oq, ok = _results(name, "out", out, (q, k))
+        _check(load_library().mslt_head_norm_rotary(
+            st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)),
+            *_gains(name, gain_q, gain_k, hq, hk, w), eps, _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
+            C.byref(_heads(name, "out", oq, q, q.shape)), C.byref(_heads(name, "out", ok, q, k.shape))))
+    return oq, ok
+
+
+def mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form: RotaryForm, grad_q, grad_k, positions=None, out=None, stream=None):
+    """Gradients of mslt_head_norm_rotary from those of its results; q, k and the gains as it got them.  out: tensors for
+    dq and dk, grad_q and grad_k themselves allowed.  Returns a dict of dq, dk, dgain_q, dgain_k.  Enqueues only."""
+    import torch
+    name = "mslt_head_norm_rotary_backward"
+    B, S, hq, hk, w = _rotary_sizes(name, q, k)
+    lib = load_library()
+    with _Place(name, stream, [q, k, gain_q, gain_k, grad_q, grad_k, positions] + list(out or ())) as st:
+        dq, dk = _results(name, "out", out, (q, k))
+        gains = _gains(name, gain_q, gain_k, hq, hk, w)
+        dgq, dgk = torch.empty_like(gain_q), torch.empty_like(gain_k)
+        need = C.c_size_t()
+        _check(lib.mslt_head_norm_workspace(B, S, hq, hk, w, C.byref(need)))
+        ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        _check(lib.mslt_head_norm_rotary_backward(
+            st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), *gains, eps,
+            _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
+            C.byref(_heads(name, "grad_q", grad_q, q, q.shape)), C.byref(_heads(name, "grad_k", grad_k, q, k.shape)),
+            C.byref(_heads(name, "out", dq, q, q.shape)), C.byref(_heads(name, "out", dk, q, k.shape)),
+            dgq.data_ptr(), dgk.data_ptr(), ws.data_ptr(), need.value))
+    return {"dq": dq, "dk": dk, "dgain_q": dgq, "dgain_k": dgk}
+
+
+def attention_form(scale=None, cap=0.0, causal=False) -> AttentionForm:
+    """How queries attend, see mslt_attention_form in the header; scale: 1/sqrt(width) unless given."""
+    if scale is not None and not scale > 0:
+        raise _refusal(f"attention_form: scale must be above 0, not {scale}")
+    return AttentionForm(0.0 if scale is None else scale, cap, int(causal), None, None, None)
+
+
+def _attention_call(name, q, k, v, form, documents, prefix, slopes):
+    """Sizes, operands and the form with its device pointers."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        raise _refusal(f"{name}: q {tuple(q.shape)} and k {tuple(k.shape)} must be [batch, rows, heads, width] of one batch and width")
+    (B, n, h, w), (S, kv) = q.shape, k.shape[1:3]
+    f = AttentionForm(form.scale or w ** -0.5, form.cap, form.causal, _flat(name, "documents", documents, torch.int32, (B, S)),
+                      _flat(name, "prefix", prefix, torch.int32, (B,)), _flat(name, "slopes", slopes, torch.float32, (h,)))
+    return ((_precision(name, q), B, n, S, h, kv, w),
+            (C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "v", v, q, k.shape))), f)
+
+
+def _attention_workspace(lib, sizes, backward, device):
+    import torch
+    need = C.c_size_t()
+    _check(lib.mslt_attention_workspace(*sizes, backward, C.byref(need)))
+    return torch.empty(need.value, dtype=torch.uint8, device=device)
+
+
+def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, slopes=None, out=None, stream=None):
+    """Attention of q [batch, queries, heads, width] over k, v [batch, keys, kv_heads, width], any strides with contiguous
+    elements; the queries are the last positions.  documents: int32 [batch, keys], negative for padding; prefix: int32 [batch];
+    slopes: fp32 [heads].  out: tensor for the result.  Returns a dict of out and lse.  Enqueues only."""
+    import torch
+    name, lib = "mslt_attention", load_library()
+    with _Place(name, stream, [q, k, v, documents, prefix, slopes, out]) as st:
+        sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
+        out, = _results(name, "out", (out,), (q,))
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        ws = _attention_workspace(lib, sizes, 0, q.device)
+        _check(lib.mslt_attention(st, *sizes, *qkv, C.byref(f), C.byref(_heads(name, "out", out, q, q.shape)), lse.data_ptr(),
+                                  ws.data_ptr(), ws.numel()))
+    return {"out": out, "lse": lse}
+
+
+def mslt_attention_backward(q, k, v, out, lse, grad_out, form: AttentionForm, documents=None, prefix=None, slopes=None, grads=None,
+                            stream=None):
+    """Gradients of mslt_attention from that of its out; operands, out and lse as it got and left them.  grads: tensors for dq, dk
+    and dv.  Returns a dict of dq, dk, dv.  Enqueues only."""
+    import torch
+    name, lib = "mslt_attention_backward", load_library()
+    with _Place(name, stream, [q, k, v, out, lse, grad_out, documents, prefix, slopes] + list(grads or ())) as st:
+        sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
+        dq, dk, dv = _results(name, "grads", grads, (q, k, v))
+        ws = _attention_workspace(lib, sizes, 1, q.device)
+        _check(lib.mslt_attention_backward(
+            st, *sizes, *qkv, C.byref(_heads(name, "out", out, q, q.shape)),
+            _flat(name, "lse", lse, torch.float32, (q.shape[0], q.shape[2], q.shape[1])),
+            C.byref(_heads(name, "grad_out", grad_out, q, q.shape)), C.byref(f), C.byref(_heads(name, "grads", dq, q, q.shape)),
+            C.byref(_heads(name, "grads", dk, q, k.shape)), C.byref(_heads(name, "grads", dv, q, k.shape)), ws.data_ptr(), ws.numel()))
+    return {"dq": dq, "dk": dk, "dv": dv}
 
 
 class Model:

@@ -1,0 +1,786 @@
+// Attention with a score cap, a distance bias, a document mask and a prefix mask, grouped key/value heads; bf16 and fp32.
+//
+//   s = scale q.k;  s <- cap tanh(s / cap);  s <- s - slope |pos_q - pos_k|;  p = softmax of s over the visible keys;  o = p v
+//
+// One pass over the keys with a running maximum and sum, in base 2 (log2 e folded into the factors).  The query heads that
+// share a key/value head are rows of the same tile: row R of a kv head is query R / G of head R % G of its group, so a key
+// or value is read once for all of them and the gradients of a shared head add up in registers, in a fixed order.
+//
+// All products are 32 x 32 matrix instructions formed transposed, so that the softmax index sits in a lane's registers:
+//   S^T[key, row] = K Q^T, O^T[d, row] = V^T P^T (lane = row);  backward likewise for dQ; for dK, dV lane = key, registers = rows.
+// An accumulator is the B operand of the next product as it stands; the A operand (V^T, K^T, Q^T, dO^T) is read transposed
+// out of the same LDS tile that the first product reads by rows.
+//
+// Which tiles a workgroup visits: tiles that no row of it can see are left out.  For documents, the least and largest
+// entry of every 64 positions are found first (k_doc_ranges); each workgroup turns them and the position limits into a
+// list of tiles.  A wavefront masks element by element only in tiles that are neither hidden from all its rows nor open
+// to all of them.
+#pragma once
+#include "common.h"
+
+#include <atomic>
+
+namespace mslt {
+namespace forms {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int LIST = 256;            // tiles listed at a time, one per thread
+constexpr float NO_MAX = -1e30f;     // running maximum before the first visible key: finite, so that differences are
+
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+// row of a 32-row block that register r of this half-wave holds, without the 4 * half
+__device__ __forceinline__ constexpr int acc_row(int r) { return 8 * (r >> 2) + (r & 3); }
+__device__ __forceinline__ int wave_min_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max_i(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// LDS tile of rows of D elements in 16-byte chunks; chunk c of a row sits in place c ^ swz(row).  The order makes both
+// ways of reading free of bank conflicts: 16 rows at one chunk (first products), and four consecutive rows at four
+// neighbouring chunks (transposed bf16 reads) or two rows four apart at 32 consecutive floats (fp32).
+template <typename T, int D>
+struct Tile {
+  static constexpr int CH = 16 / (int)sizeof(T);
+  static constexpr int CPR = D / CH;
+  static constexpr int ROWB = D * (int)sizeof(T);
+  static constexpr int NS = CPR / 2;     // 16-byte fragments of a row that one half-wave holds
+  static __device__ __forceinline__ int swz(int row) {
+    if constexpr (sizeof(T) == 4) return (row & 3) | (((row >> 2) & 1) << 3) | (((row >> 3) & 1) << 2);
+    else if constexpr (CPR == 8) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+    else return ((row & 3) << 2) | ((row >> 2) & 3);
+  }
+  static __device__ __forceinline__ u32x4_t* at(unsigned char* lds, int row, int chunk) {
+    return reinterpret_cast<u32x4_t*>(lds + row * ROWB + 16 * (chunk ^ swz(row)));
+  }
+};
+
+// a lane's 16-byte pieces of one row: half-wave h holds chunks 2 s + h
+template <typename T, int D>
+using Frags = u32x4_t[Tile<T, D>::NS];
+
+template <typename T>
+__device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t acc) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+  } else {
+    const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], y[j], acc, 0, 0, 0);
+    return acc;
+  }
+}
+// [32 tile rows from row0] x [fragment rows]: lane = fragment row, registers = tile rows
+template <typename T, int D>
+__device__ __forceinline__ f32x16_t dot_rows(unsigned char* tile, int row0, const Frags<T, D>& f, int lane) {
+  f32x16_t acc = zero16();
+  const int row = row0 + (lane & 31), half = lane >> 5;
+#pragma unroll
+  for (int s = 0; s < Tile<T, D>::NS; ++s) acc = mma<T>(*Tile<T, D>::at(tile, row, 2 * s + half), f[s], acc);
+  return acc;
+}
+// registers 8c .. 8c+7 as a B operand
+__device__ __forceinline__ bf16x8_t pack_frag(const f32x16_t& p, int c) {
+  u32x4_t u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = pack_bf16x2(p[8 * c + 2 * i], p[8 * c + 2 * i + 1]);
+  return __builtin_bit_cast(bf16x8_t, u);
+}
+// acc[d, lane's column] += sum over 32 tile rows from row0 of tile[row][d] * p[row, column].  bf16: p is rounded to bf16
+// here, the one rounding between the two products (the sum of a row is taken before it); a term is then off by 2^-9 of
+// itself, as the operands of the first product already are.
+template <typename T, int D>
+__device__ __forceinline__ void add_outer(f32x16_t (&acc)[D / 32], unsigned char* tile, int row0, const f32x16_t& p, int lane) {
+  const int half = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    const int j = lane & 15, blk = (lane >> 4) & 1;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const bf16x8_t f = pack_frag(p, c);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        s16x4_t v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          // sixteen lanes fetch four consecutive rows of sixteen d and receive four rows of one d each
+          const int row = row0 + 16 * c + 8 * i + 4 * half + (j >> 2), d = 32 * db + 16 * blk + 4 * (j & 3);
+          unsigned char* src = tile + row * Tile<T, D>::ROWB + 16 * ((d >> 3) ^ Tile<T, D>::swz(row)) + 2 * (d & 7);
+          v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)src);
+        }
+        struct { s16x4_t lo, hi; } w{v[0], v[1]};
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, w), f, acc[db], 0, 0, 0);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = row0 + acc_row(r) + 4 * half;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const int d = 32 * db + (lane & 31);
+        const float x = *reinterpret_cast<const float*>(tile + row * Tile<T, D>::ROWB + 16 * ((d >> 2) ^ Tile<T, D>::swz(row)) + 4 * (d & 3));
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[r], acc[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// Score in base 2 from the product of a query and a key, and what the gradient is multiplied by behind the cap.
+// tanh x = 1 - 2 / (1 + e^2x): absolute error a few 2^-24 for any x, and the score's is cap times that.
+struct Score {
+  float a, c;      // no cap: s2 = a * x.  cap: s2 = c * tanh, exponent a * x
+};
+template <bool CAP>
+__device__ __forceinline__ float score2(const Score& f, float x, float& damp) {
+  if constexpr (!CAP) return f.a * x;
+  const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f.a * x)), 1.f);
+  damp = fmaf(-t, t, 1.f);
+  return f.c * t;
+}
+__device__ __forceinline__ Score make_score(float scale, float cap) {
+  return cap > 0.f ? Score{2.f * LOG2E * scale / cap, cap * LOG2E} : Score{scale * LOG2E, 0.f};
+}
+
+__device__ __forceinline__ const int2* range_row(const FormArgs& a, int b) { return a.ranges + (size_t)b * ((a.S + 63) / 64); }
+
+// The workgroups of one kv head run one after the other on one XCD, whose L2 then holds its keys and values.
+__device__ __forceinline__ int xcd_order(int id, int total) {
+  const int q = total >> 3, r = total & 7, x = id & 7;
+  return x * q + min(x, r) + (id >> 3);
+}
+
+struct TileList {
+  int tile[LIST], lo[LIST], hi[LIST];
+  int count[4];
+};
+// Appends the tiles of the threads that ask for it; returns how many there are.  Called by the whole workgroup of 256.
+__device__ __forceinline__ int make_list(TileList& l, bool take, int tile, int lo, int hi, int tid) {
+  const unsigned long long m = __ballot(take);
+  const int wave = tid >> 6, lane = tid & 63;
+  __syncthreads();            // the list before this one has been read
+  if (lane == 0) l.count[wave] = __popcll(m);
+  __syncthreads();
+  int at = __popcll(m & ((1ull << lane) - 1ull)), n = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) at += l.count[w];
+    n += l.count[w];
+  }
+  if (take) {
+    l.tile[at] = tile;
+    l.lo[at] = lo;
+    l.hi[at] = hi;
+  }
+  __syncthreads();
+  return n;
+}
+
+template <typename T>
+__device__ __forceinline__ const T* head_ptr(const FormHeads& x, int b, int h) {
+  return reinterpret_cast<const T*>(x.p) + (long long)b * x.sb + (long long)h * x.sh;
+}
+template <typename T>
+__device__ __forceinline__ T* head_out(const FormHeads& x, int b, int h) {
+  return reinterpret_cast<T*>(const_cast<void*>(x.p)) + (long long)b * x.sb + (long long)h * x.sh;
+}
+
+// A lane's row of a [row, d] operand as fragments; rows that are not live and elements past the width are zeros.
+template <typename T, int D>
+__device__ __forceinline__ void load_frags(Frags<T, D>& f, const T* row, int half, int width, bool live) {
+#pragma unroll
+  for (int s = 0; s < Tile<T, D>::NS; ++s) {
+    const int e = (2 * s + half) * Tile<T, D>::CH;
+    f[s] = u32x4_t{0, 0, 0, 0};
+    if (live && e < width) f[s] = *reinterpret_cast<const u32x4_t*>(row + e);
+  }
+}
+// ROWS consecutive positions from row0 on into a tile; rows from S on, rows of padding and elements past the width as zeros
+template <typename T, int D, int ROWS>
+__device__ __forceinline__ void load_keys(unsigned char* tile, const T* base, long long stride, int row0, int S, int width,
+                                          const int32_t* docs, int tid) {
+  constexpr int CPR = Tile<T, D>::CPR;
+#pragma unroll
+  for (int i = 0; i < ROWS * CPR / 256; ++i) {
+    const int idx = tid + 256 * i, row = idx / CPR, c = idx % CPR, key = row0 + row;
+    u32x4_t v = u32x4_t{0, 0, 0, 0};
+    if (key < S && c * Tile<T, D>::CH < width && (docs == nullptr || docs[key] >= 0))
+      v = *reinterpret_cast<const u32x4_t*>(base + (long long)key * stride + c * Tile<T, D>::CH);
+    *Tile<T, D>::at(tile, row, c) = v;
+  }
+}
+
+__device__ __forceinline__ void store4(bf16* p, float a, float b, float c, float d) {
+  *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack_bf16x2(a, b), pack_bf16x2(c, d)};
+}
+__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
+  *reinterpret_cast<f32x4_t*>(p) = f32x4_t{a, b, c, d};
+}
+// accumulators [d, lane's row] to the row at p
+template <typename T, int D>
+__device__ __forceinline__ void store_row(T* p, const f32x16_t (&acc)[D / 32], int half, int width, float factor, bool live) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * db + 8 * g + 4 * half;
+      if (d >= width) continue;
+      float x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = live ? acc[db][4 * g + j] * factor : 0.f;
+      store4(p + d, x[0], x[1], x[2], x[3]);
+    }
+}
+
+// Number of keys, from the first on, among which a query at `pos` may see (of its document): its keys are 0 .. limit-1.
+__device__ __forceinline__ int key_limit(const FormArgs& a, int pos, int prefix) {
+  return a.causal ? min(a.S, max(pos + 1, prefix)) : a.S;
+}
+
+// What a lane that owns a query row knows of it.
+struct RowOf {
+  int R, qi, head, pos, id, lim;
+  bool in, live;       // inside the tensor; sees anything at all
+  float slope2;
+};
+__device__ __forceinline__ RowOf row_of(const FormArgs& a, int R, int b, int hk, int prefix) {
+  RowOf r;
+  const int G = a.nh / a.nkv;
+  r.R = R;
+  r.in = R < a.n * G;
+  const int Rc = r.in ? R : 0;
+  r.qi = Rc / G;
+  r.head = hk * G + Rc % G;
+  r.pos = a.S - a.n + r.qi;
+  r.id = a.docs ? a.docs[(size_t)b * a.S + r.pos] : 0;
+  r.live = r.in && r.id >= 0;
+  r.lim = r.live ? key_limit(a, r.pos, prefix) : 0;
+  r.slope2 = a.slopes ? a.slopes[r.head] * LOG2E : 0.f;
+  return r;
+}
+// Limits and document entries of the live rows of a wavefront, or of a workgroup.
+struct Span {
+  int lim_lo, lim_hi, id_lo, id_hi;
+};
+__device__ __forceinline__ Span wave_span(const RowOf& r) {
+  constexpr int BIG = 0x7fffffff;
+  return Span{wave_min_i(r.live ? r.lim : BIG), wave_max_i(r.lim), wave_min_i(r.live ? r.id : BIG), wave_max_i(r.live ? r.id : -1)};
+}
+__device__ __forceinline__ Span group_span(const Span& w, int (&shared)[4][4], int wave, int lane) {
+  if (lane == 0) {
+    shared[wave][0] = w.lim_lo;
+    shared[wave][1] = w.lim_hi;
+    shared[wave][2] = w.id_lo;
+    shared[wave][3] = w.id_hi;
+  }
+  __syncthreads();
+  Span s = w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s.lim_lo = min(s.lim_lo, shared[i][0]);
+    s.lim_hi = max(s.lim_hi, shared[i][1]);
+    s.id_lo = min(s.id_lo, shared[i][2]);
+    s.id_hi = max(s.id_hi, shared[i][3]);
+  }
+  return s;
+}
+// keys k0 .. k0 + count - 1 with entries lo .. hi: 0 hidden from every row of the span, 2 open to every one, 1 neither
+__device__ __forceinline__ int tile_state(const FormArgs& a, const Span& s, int k0, int count, int lo, int hi) {
+  if (k0 >= s.lim_hi) return 0;
+  if (a.docs && (hi < s.id_lo || lo > s.id_hi)) return 0;
+  if (k0 + count > s.lim_lo) return 1;
+  return a.docs && !(lo == hi && lo == s.id_lo && lo == s.id_hi) ? 1 : 2;
+}
+// least and largest document entry of the positions p0 .. p1, by whole blocks of 64 of them
+__device__ __forceinline__ void positions_range(const FormArgs& a, int b, int p0, int p1, int& lo, int& hi) {
+  lo = hi = 0;
+  if (!a.docs) return;
+  const int2* r = range_row(a, b);
+  lo = 0x7fffffff;
+  hi = -0x7fffffff;
+  for (int i = p0 >> 6; i <= p1 >> 6; ++i) {
+    lo = min(lo, r[i].x);
+    hi = max(hi, r[i].y);
+  }
+}
+
+// Scores of 32 keys from k0 on (registers) for a lane's row: cap, distance, mask.
+template <bool CAP, bool DAMP>
+__device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int half, bool mask,
+                                       f32x16_t& s, f32x16_t& damp) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float d = 1.f;
+    s[i] = score2<CAP>(f, s[i], d);
+    if constexpr (CAP && DAMP) damp[i] = d;
+  }
+  if (a.slopes) {
+    const float far = (float)(r.pos - k0 - 4 * half);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope2, fabsf(far - (float)acc_row(i)), s[i]);
+  }
+  if (mask) {
+    const int lim = r.lim - k0 - 4 * half;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = acc_row(i) < lim ? s[i] : -INFINITY;
+    if (a.docs) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int4 v = *reinterpret_cast<const int4*>(ids + 8 * g + 4 * half);
+        const int id[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * g + j] = id[j] == r.id ? s[4 * g + j] : -INFINITY;
+      }
+    }
+  }
+}
+
+// ---- forward ----------------------------------------------------------------------------------------------------------
+// FEW = false: 128 rows, 32 per wavefront, tiles of 64 keys.  FEW = true: at most 32 rows (one query and its group, or a few);
+// the four wavefronts share them, each takes 32 keys of a tile of 128, and they join their results in LDS at the end.
+// Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
+template <typename T, int D, bool FEW>
+struct Fwd {
+  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 128;
+  static constexpr int TILE = KT * Tile<T, D>::ROWB;
+  static constexpr int JOIN = FEW ? 4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 : 0;
+  static constexpr int LDS = 2 * TILE > JOIN ? 2 * TILE : JOIN;
+};
+
+template <typename T, int D, bool CAP, bool FEW>
+__global__ void __launch_bounds__(256) k_forms_fwd(FormArgs a) {
+  using F = Fwd<T, D, FEW>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  __shared__ TileList list;
+  __shared__ int span_s[4][4];
+  __shared__ __attribute__((aligned(16))) int ids[F::KT];
+  unsigned char* const Ks = lds;
+  unsigned char* const Vs = lds + F::TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + F::ROWS - 1) / F::ROWS;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int split = id % a.splits;
+  id /= a.splits;
+  const int rt = a.causal ? n_rt - 1 - id % n_rt : id % n_rt;     // the longest rows first
+  id /= n_rt;
+  const int hk = id % a.nkv, b = id / a.nkv;
+
+  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const RowOf r = row_of(a, rt * F::ROWS + (FEW ? 0 : wave * 32) + (lane & 31), b, hk, prefix);
+  const Span ws = wave_span(r), gs = group_span(ws, span_s, wave, lane);
+  const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
+  Frags<T, D> qf;
+  load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
+  const T* kbase = head_ptr<T>(a.k, b, hk);
+  const T* vbase = head_ptr<T>(a.v, b, hk);
+  const Score sc = make_score(a.scale, a.cap);
+
+  f32x16_t o[D / 32], unused;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = zero16();
+  float m_run = NO_MAX, l_run = 0.f;
+  const int n_tiles = (a.S + F::KT - 1) / F::KT, per = (n_tiles + a.splits - 1) / a.splits;
+  const int t_end = min(n_tiles, (split + 1) * per);
+  for (int base = split * per; base < t_end; base += LIST) {
+    const int t = base + tid;
+    int lo = 0, hi = 0, take = 0;
+    if (t < t_end) {
+      positions_range(a, b, t * F::KT, min(a.S, (t + 1) * F::KT) - 1, lo, hi);
+      take = tile_state(a, gs, t * F::KT, F::KT, lo, hi) != 0;
+    }
+    const int count = make_list(list, take, t, lo, hi, tid);
+    for (int i = 0; i < count; ++i) {
+      const int k0 = list.tile[i] * F::KT;
+      __syncthreads();
+      load_keys<T, D, F::KT>(Ks, kbase, a.k.sr, k0, a.S, a.w, docs, tid);
+      load_keys<T, D, F::KT>(Vs, vbase, a.v.sr, k0, a.S, a.w, docs, tid);
+      if (docs && tid < F::KT) ids[tid] = k0 + tid < a.S ? docs[k0 + tid] : -1;
+      __syncthreads();
+      const int state = tile_state(a, ws, k0, F::KT, list.lo[i], list.hi[i]);
+      if (state == 0) continue;
+#pragma unroll 1
+      for (int kb = FEW ? wave : 0; kb < (FEW ? wave + 1 : F::KT / 32); ++kb) {
+        f32x16_t s = dot_rows<T, D>(Ks, 32 * kb, qf, lane);
+        scores<CAP, false>(a, sc, r, ids + 32 * kb, k0 + 32 * kb, half, state == 1, s, unused);
+        float top = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          s[j] = __builtin_amdgcn_exp2f(s[j] - m_new);
+          sum += s[j];
+        }
+        l_run = l_run * alpha + sum;
+        m_run = m_new;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) o[db][j] *= alpha;
+        add_outer<T, D>(o, Vs, 32 * kb, s, lane);
+      }
+    }
+  }
+  l_run += __shfl_xor(l_run, 32, 64);
+
+  if constexpr (FEW) {
+    // the four wavefronts' results of each row: put onto the largest maximum and added, wavefront by wavefront
+    constexpr int LD = D + 4;
+    float* const po = reinterpret_cast<float*>(lds);
+    float* const pm = po + 4 * 32 * LD;
+    float* const pl = pm + 4 * 32;
+    __syncthreads();
+    if (half == 0) {
+      pm[wave * 32 + lane] = m_run;
+      pl[wave * 32 + lane] = l_run;
+    }
+    store_row<float, D>(po + (wave * 32 + (lane & 31)) * LD, o, half, D, 1.f, true);
+    __syncthreads();
+    // (each wavefront takes 8 rows, 8 lanes a row)
+    const int row = wave * 8 + (lane >> 3), R = rt * F::ROWS + row;
+    float m = NO_MAX, l = 0.f, e[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, pm[w * 32 + row]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      e[w] = __builtin_amdgcn_exp2f(pm[w * 32 + row] - m);
+      l += e[w] * pl[w * 32 + row];
+    }
+    const RowOf rr = row_of(a, R, b, hk, prefix);
+    if (!rr.in) return;
+    const bool some = rr.live && l > 0.f;
+    const size_t prow = ((size_t)split * a.B * a.nkv + (size_t)b * a.nkv + hk) * rows + R;
+    const float inv = a.splits > 1 ? 1.f : some ? 1.f / l : 0.f;
+    T* const out = head_out<T>(a.o, b, rr.head) + (long long)rr.qi * a.o.sr;
+    for (int d = 4 * (lane & 7); d < a.w; d += 32) {
+      f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) x += *reinterpret_cast<const f32x4_t*>(po + (w * 32 + row) * LD + d) * e[w];
+      x *= inv;
+      if (a.splits > 1) *reinterpret_cast<f32x4_t*>(a.part + prow * a.w + d) = x;
+      else store4(out + d, some ? x[0] : 0.f, some ? x[1] : 0.f, some ? x[2] : 0.f, some ? x[3] : 0.f);
+    }
+    if ((lane & 7) == 0) {
+      if (a.splits > 1) a.part_ml[prow] = make_float2(m, rr.live ? l : 0.f);
+      else a.lse[((size_t)b * a.nh + rr.head) * a.n + rr.qi] = some ? (m + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+    }
+  } else {
+    if (!r.in) return;
+    const bool some = r.live && l_run > 0.f;
+    if (a.splits > 1) {
+      const size_t prow = ((size_t)split * a.B * a.nkv + (size_t)b * a.nkv + hk) * rows + r.R;
+      store_row<float, D>(a.part + prow * a.w, o, half, a.w, 1.f, true);
+      if (half == 0) a.part_ml[prow] = make_float2(m_run, r.live ? l_run : 0.f);
+    } else {
+      store_row<T, D>(head_out<T>(a.o, b, r.head) + (long long)r.qi * a.o.sr, o, half, a.w, some ? 1.f / l_run : 0.f, some);
+      if (half == 0) a.lse[((size_t)b * a.nh + r.head) * a.n + r.qi] = some ? (m_run + __builtin_amdgcn_logf(l_run)) * LN2 : -INFINITY;
+    }
+  }
+}
+
+// Results of the workgroups that shared a row's keys: put onto the largest maximum, added in their order.  One wavefront a row.
+template <typename T>
+__global__ void __launch_bounds__(256) k_forms_join(FormArgs a) {
+  const int lane = threadIdx.x & 63, G = a.nh / a.nkv, rows = a.n * G;
+  const size_t total = (size_t)a.B * a.nkv * rows, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= total) return;
+  float m = NO_MAX, l = 0.f;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[s * total + row].x);
+  f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int d = 4 * lane;
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = a.part_ml[s * total + row];
+    const float e = __builtin_amdgcn_exp2f(ml.x - m);
+    l += e * ml.y;
+    if (d < a.w && ml.y > 0.f) x += *reinterpret_cast<const f32x4_t*>(a.part + (s * total + row) * a.w + d) * e;
+  }
+  const int R = (int)(row % rows), hk = (int)(row / rows) % a.nkv, b = (int)(row / ((size_t)rows * a.nkv));
+  const int head = hk * G + R % G, qi = R / G;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if (d < a.w) store4(head_out<T>(a.o, b, head) + (long long)qi * a.o.sr + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  if (lane == 0) a.lse[((size_t)b * a.nh + head) * a.n + qi] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+}
+
+// ---- backward, query side: delta = sum_d dO O, dQ -----------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
+  float s = 0.f;
+  if constexpr (sizeof(T) == 2) {
+    const bf16x8_t u = __builtin_bit_cast(bf16x8_t, x), v = __builtin_bit_cast(bf16x8_t, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf((float)u[i], (float)v[i], s);
+  } else {
+    const f32x4_t u = __builtin_bit_cast(f32x4_t, x), v = __builtin_bit_cast(f32x4_t, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fmaf(u[i], v[i], s);
+  }
+  return s;
+}
+
+template <typename T, int D, bool CAP>
+__global__ void __launch_bounds__(256) k_forms_bwd_q(FormArgs a) {
+  constexpr int KT = 64, TILE = KT * Tile<T, D>::ROWB;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  __shared__ TileList list;
+  __shared__ int span_s[4][4];
+  __shared__ __attribute__((aligned(16))) int ids[KT];
+  unsigned char* const Ks = lds;
+  unsigned char* const Vs = lds + TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + 127) / 128;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int rt = a.causal ? n_rt - 1 - id % n_rt : id % n_rt;
+  id /= n_rt;
+  const int hk = id % a.nkv, b = id / a.nkv;
+
+  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const RowOf r = row_of(a, rt * 128 + wave * 32 + (lane & 31), b, hk, prefix);
+  const Span ws = wave_span(r), gs = group_span(ws, span_s, wave, lane);
+  const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
+  const T* kbase = head_ptr<T>(a.k, b, hk);
+  const T* vbase = head_ptr<T>(a.v, b, hk);
+  const Score sc = make_score(a.scale, a.cap);
+
+  Frags<T, D> qf, gf;
+  const size_t lrow = ((size_t)b * a.nh + r.head) * a.n + r.qi;
+  float l2 = INFINITY, delta = 0.f;
+  if (r.live) {
+    l2 = a.lse[lrow] * LOG2E;
+    if (l2 == -INFINITY) l2 = INFINITY;       // sees no key: probabilities zero
+  }
+  load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
+  load_frags<T, D>(gf, head_ptr<T>(a.g, b, r.head) + (long long)r.qi * a.g.sr, half, a.w, r.live);
+  {
+    Frags<T, D> of;
+    load_frags<T, D>(of, head_ptr<T>(a.o, b, r.head) + (long long)r.qi * a.o.sr, half, a.w, r.live);
+#pragma unroll
+    for (int s = 0; s < Tile<T, D>::NS; ++s) delta += dot_chunk<T>(gf[s], of[s]);
+    delta += __shfl_xor(delta, 32, 64);
+    if (r.in && half == 0) a.delta[lrow] = delta;
+  }
+
+  f32x16_t dq[D / 32], damp;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dq[i] = zero16();
+  const int n_tiles = (a.S + KT - 1) / KT;
+  for (int base = 0; base < n_tiles; base += LIST) {
+    const int t = base + tid;
+    int lo = 0, hi = 0, take = 0;
+    if (t < n_tiles) {
+      positions_range(a, b, t * KT, min(a.S, (t + 1) * KT) - 1, lo, hi);
+      take = tile_state(a, gs, t * KT, KT, lo, hi) != 0;
+    }
+    const int count = make_list(list, take, t, lo, hi, tid);
+    for (int i = 0; i < count; ++i) {
+      const int k0 = list.tile[i] * KT;
+      __syncthreads();
+      load_keys<T, D, KT>(Ks, kbase, a.k.sr, k0, a.S, a.w, docs, tid);
+      load_keys<T, D, KT>(Vs, vbase, a.v.sr, k0, a.S, a.w, docs, tid);
+      if (docs && tid < KT) ids[tid] = k0 + tid < a.S ? docs[k0 + tid] : -1;
+      __syncthreads();
+      const int state = tile_state(a, ws, k0, KT, list.lo[i], list.hi[i]);
+      if (state == 0) continue;
+#pragma unroll 1
+      for (int kb = 0; kb < KT / 32; ++kb) {
+        f32x16_t s = dot_rows<T, D>(Ks, 32 * kb, qf, lane);
+        f32x16_t dp = dot_rows<T, D>(Vs, 32 * kb, gf, lane);
+        scores<CAP, true>(a, sc, r, ids + 32 * kb, k0 + 32 * kb, half, state == 1, s, damp);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          s[j] = __builtin_amdgcn_exp2f(s[j] - l2) * (dp[j] - delta);
+          if constexpr (CAP) s[j] *= damp[j];
+        }
+        add_outer<T, D>(dq, Ks, 32 * kb, s, lane);
+      }
+    }
+  }
+  if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
+}
+
+// ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
+// 128 keys, 32 per wavefront, over tiles of 64 rows of the group's heads.
+template <typename T, int D, bool CAP>
+__global__ void __launch_bounds__(256) k_forms_bwd_kv(FormArgs a) {
+  constexpr int RT = 64, TILE = RT * Tile<T, D>::ROWB, CPR = Tile<T, D>::CPR;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  __shared__ TileList list;
+  __shared__ __attribute__((aligned(16))) float l2_s[RT], delta_s[RT], slope_s[RT];
+  __shared__ __attribute__((aligned(16))) int lim_s[RT], id_s[RT], pos_s[RT];
+  unsigned char* const Qs = lds;
+  unsigned char* const Gs = lds + TILE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int G = a.nh / a.nkv, rows = a.n * G, n_kt = (a.S + 127) / 128, first = a.S - a.n;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int kt = id % n_kt;
+  id /= n_kt;
+  const int hk = id % a.nkv, b = id / a.nkv;
+  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
+  const int kw = kt * 128 + wave * 32, key = kw + (lane & 31);      // this wavefront's keys, this lane's
+  const bool in = key < a.S;
+  const int kid = docs ? (in ? docs[key] : -1) : 0;
+  const bool live = in && kid >= 0;
+  const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
+  const Score sc = make_score(a.scale, a.cap);
+  int klo, khi;
+  positions_range(a, b, kt * 128, min(a.S, kt * 128 + 128) - 1, klo, khi);
+
+  Frags<T, D> kf, vf;
+  load_frags<T, D>(kf, head_ptr<T>(a.k, b, hk) + (long long)(in ? key : 0) * a.k.sr, half, a.w, live);
+  load_frags<T, D>(vf, head_ptr<T>(a.v, b, hk) + (long long)(in ? key : 0) * a.v.sr, half, a.w, live);
+  f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
+
+  const int n_tiles = (rows + RT - 1) / RT;
+  for (int base = 0; base < n_tiles; base += LIST) {
+    const int t = base + tid;
+    int lo = 0, hi = 0, take = 0;
+    if (t < n_tiles) {
+      const int p0 = first + t * RT / G, p1 = first + min(rows - 1, t * RT + RT - 1) / G;
+      positions_range(a, b, p0, p1, lo, hi);
+      take = kt * 128 < key_limit(a, p1, prefix) && (!docs || (hi >= 0 && khi >= 0 && lo <= khi && hi >= klo));
+    }
+    const int count = make_list(list, take, t, lo, hi, tid);
+    for (int i = 0; i < count; ++i) {
+      const int R0 = list.tile[i] * RT, p0 = first + R0 / G, p1 = first + min(rows - 1, R0 + RT - 1) / G;
+      const int lo_t = list.lo[i], hi_t = list.hi[i];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < RT * CPR / 256; ++j) {
+        const int idx = tid + 256 * j, row = idx / CPR, c = idx % CPR, R = R0 + row;
+        u32x4_t q = u32x4_t{0, 0, 0, 0}, g = q;
+        if (R < rows && c * Tile<T, D>::CH < a.w) {
+          const int qi = R / G, head = hk * G + R % G;
+          if (!docs || docs[first + qi] >= 0) {
+            q = *reinterpret_cast<const u32x4_t*>(head_ptr<T>(a.q, b, head) + (long long)qi * a.q.sr + c * Tile<T, D>::CH);
+            g = *reinterpret_cast<const u32x4_t*>(head_ptr<T>(a.g, b, head) + (long long)qi * a.g.sr + c * Tile<T, D>::CH);
+          }
+        }
+        *Tile<T, D>::at(Qs, row, c) = q;
+        *Tile<T, D>::at(Gs, row, c) = g;
+      }
+      if (tid < RT) {
+        const RowOf r = row_of(a, R0 + tid, b, hk, prefix);
+        const size_t lrow = ((size_t)b * a.nh + r.head) * a.n + r.qi;
+        const float l2 = r.live ? a.lse[lrow] * LOG2E : INFINITY;
+        l2_s[tid] = l2 == -INFINITY ? INFINITY : l2;
+        delta_s[tid] = r.live ? a.delta[lrow] : 0.f;
+        slope_s[tid] = r.slope2;
+        lim_s[tid] = r.lim;
+        id_s[tid] = r.id;
+        pos_s[tid] = r.pos;
+      }
+      __syncthreads();
+      if (kw >= key_limit(a, p1, prefix) || kid_hi < 0) continue;
+      if (docs && (hi_t < kid_lo || lo_t > kid_hi)) continue;
+      const bool mask = kw + 32 > key_limit(a, p0, prefix) || (docs && !(lo_t == hi_t && lo_t == kid_lo && lo_t == kid_hi));
+#pragma unroll 1
+      for (int rb = 0; rb < RT / 32; ++rb) {
+        f32x16_t s = dot_rows<T, D>(Qs, 32 * rb, kf, lane);
+        f32x16_t dp = dot_rows<T, D>(Gs, 32 * rb, vf, lane);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int at = 32 * rb + 8 * g + 4 * half;
+          const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(l2_s + at), dl = *reinterpret_cast<const f32x4_t*>(delta_s + at);
+          f32x4_t sl = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          int4 ps = make_int4(0, 0, 0, 0);
+          if (a.slopes) {
+            sl = *reinterpret_cast<const f32x4_t*>(slope_s + at);
+            ps = *reinterpret_cast<const int4*>(pos_s + at);
+          }
+          const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
+          int4 lm = make_int4(0, 0, 0, 0), qi = lm;
+          if (mask) {
+            lm = *reinterpret_cast<const int4*>(lim_s + at);
+            qi = *reinterpret_cast<const int4*>(id_s + at);
+          }
+          const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float d = 1.f, x = score2<CAP>(sc, s[4 * g + j], d);
+            if (a.slopes) x = fmaf(-sl[j], fabsf((float)(pos[j] - key)), x);
+            if (mask) x = key < lim[j] && (!docs || qid[j] == kid) ? x : -INFINITY;
+            const float p = __builtin_amdgcn_exp2f(x - l2[j]);
+            s[4 * g + j] = p;
+            dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * d;
+          }
+        }
+        add_outer<T, D>(dv, Gs, 32 * rb, s, lane);
+        add_outer<T, D>(dk, Qs, 32 * rb, dp, lane);
+      }
+    }
+  }
+  if (!in) return;
+  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, a.scale, live);
+  store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)key * a.dv.sr, dv, half, a.w, 1.f, live);
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------
+template <auto Kernel>
+inline hipError_t launch(size_t blocks, int lds, const FormArgs& a, hipStream_t s) {
+  static std::atomic<bool> allowed[64];      // once per kernel and device: more than 64 KB of LDS has to be asked for
+  if (lds > 0) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64 || !allowed[dev].load(std::memory_order_relaxed)) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(Kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      if (e != hipSuccess) return e;
+      if (dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
+    }
+  }
+  Kernel<<<dim3((unsigned)blocks), dim3(256), lds, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D, bool CAP>
+hipError_t fwd_w(const FormArgs& a, hipStream_t s) {
+  const int rows = a.n * (a.nh / a.nkv);
+  const size_t heads = (size_t)a.B * a.nkv * a.splits;
+  hipError_t e = rows <= 32 ? launch<k_forms_fwd<T, D, CAP, true>>(heads, Fwd<T, D, true>::LDS, a, s)
+                            : launch<k_forms_fwd<T, D, CAP, false>>(heads * ((rows + 127) / 128), Fwd<T, D, false>::LDS, a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  return launch<k_forms_join<T>>(((size_t)a.B * a.nkv * rows + 3) / 4, 0, a, s);
+}
+template <typename T, int D, bool CAP>
+hipError_t bwd_w(const FormArgs& a, hipStream_t s) {
+  const int rows = a.n * (a.nh / a.nkv);
+  const size_t heads = (size_t)a.B * a.nkv;
+  constexpr int LDS = 2 * 64 * Tile<T, D>::ROWB;
+  const hipError_t e = launch<k_forms_bwd_q<T, D, CAP>>(heads * ((rows + 127) / 128), LDS, a, s);
+  if (e != hipSuccess) return e;
+  return launch<k_forms_bwd_kv<T, D, CAP>>(heads * ((a.S + 127) / 128), LDS, a, s);
+}
+template <typename T>
+hipError_t fwd_t(const FormArgs& a, hipStream_t s) {
+  if (a.w <= 64) return a.cap > 0.f ? fwd_w<T, 64, true>(a, s) : fwd_w<T, 64, false>(a, s);
+  return a.cap > 0.f ? fwd_w<T, 128, true>(a, s) : fwd_w<T, 128, false>(a, s);
+}
+template <typename T>
+hipError_t bwd_t(const FormArgs& a, hipStream_t s) {
+  if (a.w <= 64) return a.cap > 0.f ? bwd_w<T, 64, true>(a, s) : bwd_w<T, 64, false>(a, s);
+  return a.cap > 0.f ? bwd_w<T, 128, true>(a, s) : bwd_w<T, 128, false>(a, s);
+}
+
+}  // namespace forms
+}  // namespace mslt

@@ -247,6 +247,48 @@ bool attention_mfma_supported(int S, int dh);
 hipError_t attention_fwd_mfma(const AttnDesc& d, hipStream_t s);
 hipError_t attention_bwd_mfma(const AttnBwdDesc& d, hipStream_t s);
 
+// ---- operators between a layer's QKV projection and its output projection ----------------------
+// Heads in device memory, strides in elements: element i of head h of token t of sequence b at p + b*sb + t*sr + h*sh + i.
+struct FormHeads {
+  const void* p = nullptr;
+  long long sb = 0, sr = 0, sh = 0;
+};
+// Attention with a score cap, a distance bias, a document mask and a prefix mask (attention_forms.h).
+struct FormArgs {
+  FormHeads q, k, v, o, g, dq, dk, dv;   // g: gradient of o
+  float* lse = nullptr;                  // [B, nh, n]
+  float* delta = nullptr;                // scratch [B, nh, n]
+  const int32_t* docs = nullptr;         // [B, S] or null
+  const int32_t* prefix = nullptr;       // [B] or null
+  const float* slopes = nullptr;         // [nh] or null
+  int2* ranges = nullptr;                // scratch [B, ceil(S / 64)]: least and largest of docs in each 64 positions
+  float* part = nullptr;                 // scratch of split keys: [splits, B, nkv, rows, w], and maximum and sum
+  float2* part_ml = nullptr;
+  int B = 0, n = 0, S = 0, nh = 0, nkv = 0, w = 0, causal = 0, splits = 1;
+  float scale = 1.f, cap = 0.f;
+};
+// Parts the forward splits the keys into.
+int form_splits(int dtype, int B, int n, int S, int nh, int nkv, int w);
+hipError_t form_ranges(const FormArgs& a, hipStream_t s);
+hipError_t form_fwd_bf16(const FormArgs& a, hipStream_t s);
+hipError_t form_fwd_f32(const FormArgs& a, hipStream_t s);
+hipError_t form_bwd_bf16(const FormArgs& a, hipStream_t s);
+hipError_t form_bwd_f32(const FormArgs& a, hipStream_t s);
+
+// Rotary positions, alone or behind the norm of each head (rotary.hip).
+constexpr int ROTARY_PAIRS = 128;
+struct RotaryArgs {
+  FormHeads q, k, gq, gk, oq, ok;        // inputs, gradients of the outputs (backward), results
+  const float *gain_q = nullptr, *gain_k = nullptr;   // null: no norm
+  const int32_t* positions = nullptr;    // [B, S] or null
+  float *dgain_q = nullptr, *dgain_k = nullptr, *partial = nullptr;
+  int B = 0, S = 0, hq = 0, hk = 0, w = 0, pairs = 0, interleaved = 0, inverse = 0, per_head = 0;
+  float eps = 0.f, magnitude = 1.f;
+  unsigned long long freq[ROTARY_PAIRS] = {};   // turns per position, in 2^-64
+};
+size_t rotary_partial_floats(long long tokens, int heads, int w);
+hipError_t rotary_run(int dtype, const RotaryArgs& a, bool backward, hipStream_t s);
+
 // ---- row-wise and element-wise kernels ------------------------------------------------------
 hipError_t fill_zero(void* p, size_t bytes, hipStream_t s);
 hipError_t cast_f32_to_bf16(const float* src, bf16* dst, size_t n, hipStream_t s);

@@ -5,6 +5,7 @@
 // validates, lays out memory and enqueues.
 #include "../../include/mslt.h"
 #include "common.h"
+#include "host.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -16,7 +17,7 @@
 using namespace mslt;
 
 static thread_local std::string g_err;
-static int fail(int code, const char* fmt, ...) {
+int mslt::fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -25,12 +26,6 @@ static int fail(int code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
-#define HIP_TRY(expr)                                                                       \
-  do {                                                                                      \
-    hipError_t e__ = (expr);                                                                \
-    if (e__ != hipSuccess) return fail(MSLT_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e__)); \
-  } while (0)
-
 static inline size_t rup(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 enum { T_WORD = 0, T_POS, T_TYPE, T_ELN_G, T_ELN_B, N_EMB };

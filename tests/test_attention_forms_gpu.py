@@ -1,0 +1,205 @@
+"""mslt_attention and its gradients against the definition in float64: caps, distance biases, document and prefix masks, grouped
+heads, few queries over many keys, odd lengths and widths, layouts, padding that holds NaN, streams, graphs.
+
+Bounds are derived in forms_reference: fp32 roundings of every term, and in bf16 mode half a step (2^-8 of the value) for the
+probabilities, for dS, for the stored output that delta is taken from, and for each result."""
+import pytest
+
+from paper_2011_13635_amd import binding
+import forms_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def _documents(torch, B, S, kind, seed):
+    g = torch.Generator().manual_seed(seed)
+    if kind == "packed":       # several in a row, padding behind them; the last sequence is padding alone
+        ids = torch.sort(torch.randint(0, 4, (B, S), generator=g), 1).values
+        ids[:, S - S // 5:] = -1
+        if B > 1:
+            ids[-1] = -1
+    elif kind == "mixed":      # in no order, entries far apart, padding in between
+        ids = torch.randint(0, 3, (B, S), generator=g) * 1_000_003
+        ids[torch.rand(B, S, generator=g) < 0.2] = -7
+    else:                      # front: padded in front, as a cache is
+        ids = torch.zeros(B, S, dtype=torch.long)
+        ids[:, :S // 3] = -1
+    return ids.to(torch.int32).cuda()
+
+
+def _case(torch, dtype, B, n, S, h, kv, w, *, cap=0.0, causal=False, documents=None, prefix=False, slopes=False, backward=True, seed=0,
+          sharp=1.5, nan_padding=False):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)
+    qkv = torch.randn((B, S, (h + 2 * kv) * w), generator=g, device="cuda")
+    qkv[..., :(h + kv) * w] *= sharp
+    qkv = qkv.to(dtype)
+    q = qkv[:, S - n:, :h * w].view(B, n, h, w)
+    k = qkv[..., h * w:(h + kv) * w].view(B, S, kv, w)
+    v = qkv[..., (h + kv) * w:].view(B, S, kv, w)
+    grad = rand(B, n, h, w)
+    masks = {"documents": _documents(torch, B, S, documents, seed) if documents else None,
+             "prefix": torch.randint(-2, S + 3, (B,), generator=g, device="cuda", dtype=torch.int32) if prefix else None,
+             "slopes": (torch.rand(h, generator=g, device="cuda") - 0.2) * 16.0 / S if slopes else None}
+    if nan_padding:
+        dead = masks["documents"] < 0
+        qkv[dead] = float("nan")
+        grad[dead[:, S - n:]] = float("inf")
+    f = binding.mslt_attention(q, k, v, binding.attention_form(cap=cap, causal=causal), **masks)
+    want, lse = R.attention(q, k, v, cap=cap, causal=causal, grad=grad if backward else None, **masks)
+    got = dict(f)
+    if backward:
+        got.update(binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], grad, binding.attention_form(cap=cap, causal=causal), **masks))
+    torch.cuda.synchronize()
+    for name, w3 in want.items():
+        R.check(got[name], w3, dtype == torch.bfloat16, name)
+    empty = torch.isinf(lse)
+    assert torch.equal(empty, torch.isinf(f["lse"])) and (f["lse"][empty] < 0).all()
+    # score terms add up to at most a few hundred here: 2^-12 is 16 roundings of one of 2^8
+    assert ((f["lse"].double() - lse)[~empty].abs() <= 2.0 ** -12).all()
+    return got
+
+
+SHAPES = [
+    # B, queries, keys, heads, kv_heads, width
+    (1, 1, 1, 1, 1, 8), (2, 1, 1, 4, 2, 64), (1, 2, 3, 2, 1, 64), (2, 31, 31, 2, 2, 32), (1, 33, 33, 3, 1, 64), (2, 64, 64, 2, 2, 128),
+    (1, 65, 65, 4, 2, 80), (1, 127, 129, 2, 1, 96), (2, 128, 128, 2, 2, 64), (1, 200, 257, 6, 2, 64), (1, 130, 130, 5, 1, 120),
+    (1, 1, 1000, 8, 2, 128), (3, 1, 777, 12, 12, 64), (2, 4, 515, 8, 1, 64), (1, 5, 300, 16, 2, 128), (1, 300, 300, 1, 1, 16),
+]
+FORMS = [
+    {}, {"cap": 10.0}, {"causal": True}, {"documents": "packed"}, {"slopes": True}, {"causal": True, "prefix": True, "cap": 20.0},
+    {"documents": "mixed", "cap": 5.0, "slopes": True}, {"documents": "mixed", "causal": True, "prefix": True, "slopes": True},
+    {"documents": "front", "causal": True},
+]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("form", range(len(FORMS)))
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_attention_against_the_definition(shape, form, dtype):
+    import torch
+    _case(torch, getattr(torch, dtype), *shape, seed=form, **FORMS[form])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(1, 33, 16500, 1, 1, 8), (1, 2100, 2100, 8, 1, 16), (256, 1, 32900, 1, 1, 8), (1, 700, 2200, 2, 1, 64)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_more_tiles_than_one_list_holds(shape, dtype):
+    import torch
+    _case(torch, getattr(torch, dtype), *shape, documents="packed" if shape[2] < 4000 else None, causal=True, backward=shape[0] == 1)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(2, 150, 150, 4, 2, 64), (2, 20, 150, 2, 1, 128), (2, 1, 300, 4, 1, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_padding_may_hold_anything(shape, dtype):
+    import torch
+    for kind in ("packed", "mixed", "front"):
+        got = _case(torch, getattr(torch, dtype), *shape, documents=kind, nan_padding=True, cap=8.0, slopes=True)
+        dead = _documents(torch, shape[0], shape[2], kind, 0) < 0
+        for name in ("dk", "dv"):
+            assert (got[name][dead] == 0).all()
+        for name in ("out", "dq"):
+            assert (got[name][dead[:, shape[2] - shape[1]:]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_large_scores_stay_finite(dtype):
+    import torch
+    # scores of some thousands without a cap: one key takes a row; with a cap the tanh saturates at both ends
+    for cap in (0.0, 30.0):
+        dt = getattr(torch, dtype)
+        g = torch.Generator(device="cuda").manual_seed(1)
+        q, k, v, go = (torch.randn((1, 70, 2, 64), generator=g, device="cuda").mul(s).to(dt) for s in (60, 60, 1, 1))
+        form = binding.attention_form(cap=cap)
+        f = binding.mslt_attention(q, k, v, form)
+        d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form)
+        want, _ = R.attention(q, k, v, cap=cap, grad=go)
+        for name, w3 in want.items():
+            R.check({**f, **d}[name], w3, dt == torch.bfloat16, name)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_layouts(dtype):
+    """Heads before tokens, rows apart, a batch that is broadcast, results into parts of a packed tensor: the same values."""
+    import torch
+    dt = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    B, S, h, kv, w = 2, 90, 4, 2, 64
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda").to(dt) for s in ((B, S, h, w), (1, S, kv, w), (B, S, kv, w), (B, S, h, w)))
+    k = k.expand(B, S, kv, w)
+    form = binding.attention_form(cap=15.0, causal=True)
+    f = binding.mslt_attention(q, k.contiguous(), v, form)
+    d = binding.mslt_attention_backward(q, k.contiguous(), v, f["out"], f["lse"], go, form)
+    head_major = lambda x: x.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    apart = torch.zeros(B, S + 3, h, w + 16, dtype=dt, device="cuda")
+    apart[:, :S, :, :w] = go
+    packed = torch.full((B, S + 1, (h + 2 * kv) * w), 7.0, dtype=dt, device="cuda")
+    part = lambda at, heads: packed[:, :S, at * w:(at + heads) * w].view(B, S, heads, w)
+    out2 = torch.full((B, h, S + 1, w), 7.0, dtype=dt, device="cuda")
+    f2 = binding.mslt_attention(head_major(q), k, head_major(v), form, out=out2[:, :, :S].permute(0, 2, 1, 3))
+    d2 = binding.mslt_attention_backward(head_major(q), k, head_major(v), f2["out"], f2["lse"], apart[:, :S, :, :w], form,
+                                         grads=(part(0, h), part(h, kv), part(h + kv, kv)))
+    for name, want in {**f, **d}.items():
+        assert torch.equal({**f2, **d2}[name], want), name
+    assert (packed[:, S:] == 7).all() and (out2[:, :, S:] == 7).all()        # rows behind the last one stay as they were
+
+
+@pytest.mark.parametrize("n", [1, 90])
+def test_same_values_every_time_on_any_stream_and_in_graphs(n):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+    B, S, h, kv, w = 2, 1500, 4, 2, 64
+    q, go = (torch.randn((B, n, h, w), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn((B, S, kv, w), generator=g, device="cuda").bfloat16() for _ in range(2))
+    docs = _documents(torch, B, S, "front", 0)
+    form = binding.attention_form(cap=30.0, causal=True)
+
+    def step(**kw):
+        f = binding.mslt_attention(q, k, v, form, documents=docs, **kw)
+        return {**f, **binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form, documents=docs, **kw)}
+
+    want = {name: t.clone() for name, t in step().items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    for name in want:
+        assert torch.equal(got[name], want[name]), name
+    graphs = []
+    for _ in range(2):          # two graphs of the same operands, replayed in turn
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            res = step()
+        graphs.append((graph, res))
+    for i in range(6):
+        graph, res = graphs[i % 2]
+        for t in res.values():
+            t.fill_(3.0)
+        graph.replay()
+        eager = step()
+        torch.cuda.synchronize()
+        for name in want:
+            assert torch.equal(res[name], want[name]) and torch.equal(eager[name], want[name]), name
+
+
+def test_gradients_against_differences():
+    """fp32, a cap, a bias and masks together: the gradients against central differences of the output in float64."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(7)
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda") for s in ((1, 9, 2, 8), (1, 12, 1, 8), (1, 12, 1, 8), (1, 9, 2, 8)))
+    masks = {"documents": torch.tensor([[0, 0, 0, 0, 0, 1, 1, 1, 1, 1, 1, -1]], dtype=torch.int32, device="cuda"),
+             "prefix": torch.tensor([7], dtype=torch.int32, device="cuda"), "slopes": torch.tensor([0.1, -0.05], device="cuda")}
+    kw = {"cap": 3.0, "causal": True}
+    form = binding.attention_form(**kw)
+    f = binding.mslt_attention(q, k, v, form, **masks)
+    d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form, **masks)
+    loss = lambda *x: (R.attention(*x, **kw, **masks)[0]["out"][0] * go.double()).sum()
+    x = [t.double() for t in (q, k, v)]
+    step = 2.0 ** -13        # differences are off by its square, 2^-26, times third derivatives of order ten
+    for i, name in enumerate(("dq", "dk", "dv")):
+        for e in range(0, x[i].numel(), 5):
+            hi, lo = [t.clone() for t in x], [t.clone() for t in x]
+            hi[i].view(-1)[e] += step
+            lo[i].view(-1)[e] -= step
+            slope = ((loss(*hi) - loss(*lo)) / (2 * step)).item()
+            assert abs(d[name].reshape(-1)[e].item() - slope) < 2.0 ** -16, (name, e)
