@@ -212,19 +212,43 @@ __device__ __forceinline__ void load_frags(Frags<T, D>& f, const T* row, int hal
     if (live && e < width) f[s] = *reinterpret_cast<const u32x4_t*>(row + e);
   }
 }
-// ROWS consecutive positions from row0 on into a tile; rows from S on, rows of padding and elements past the width as zeros
+// Rows go from memory into a tile directly, 64 lanes x 16 bytes an instruction to 1024 consecutive bytes of LDS; which piece a
+// lane fetches is free, which is where the swizzle lives.  A lane whose piece is none of the operand's (a row past the end, a
+// row of padding, elements past the width) fetches beyond the buffer's end, which writes zeros.
+constexpr uint32_t NOWHERE = 0x80000000u;
+typedef __attribute__((address_space(3))) void lds_void_t;
 template <typename T, int D, int ROWS>
-__device__ __forceinline__ void load_keys(unsigned char* tile, const T* base, long long stride, int row0, int S, int width,
-                                          const int32_t* docs, int tid) {
-  constexpr int CPR = Tile<T, D>::CPR;
+struct Loader {
+  static constexpr int CPR = Tile<T, D>::CPR, NI = ROWS * CPR / 256;
+  uint32_t voff[NI];
+  static __device__ __forceinline__ int row_at(int j, int tid) { return (64 * ((tid >> 6) * NI + j) + (tid & 63)) / CPR; }
+  // row r of the tile lies (r / group) * row_bytes + (r % group) * head_bytes behind the base; rows from `used` on are none
+  __device__ __forceinline__ void init(int tid, long long row_bytes, int group, long long head_bytes, int used, int width) {
 #pragma unroll
-  for (int i = 0; i < ROWS * CPR / 256; ++i) {
-    const int idx = tid + 256 * i, row = idx / CPR, c = idx % CPR, key = row0 + row;
-    u32x4_t v = u32x4_t{0, 0, 0, 0};
-    if (key < S && c * Tile<T, D>::CH < width && (docs == nullptr || docs[key] >= 0))
-      v = *reinterpret_cast<const u32x4_t*>(base + (long long)key * stride + c * Tile<T, D>::CH);
-    *Tile<T, D>::at(tile, row, c) = v;
+    for (int j = 0; j < NI; ++j) {
+      const int r = row_at(j, tid), chunk = (tid & (CPR - 1)) ^ Tile<T, D>::swz(r);
+      const bool in = chunk * Tile<T, D>::CH < width && r < used;
+      voff[j] = in ? (uint32_t)((r / group) * row_bytes + (r % group) * head_bytes) + 16 * chunk : NOWHERE;
+    }
   }
+  template <typename Keep>
+  __device__ __forceinline__ void issue(const T* base, unsigned char* tile, int tid, bool guard, Keep keep) const {
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, 0x7fffffff, 0x00020000);
+    unsigned char* const dst = tile + (tid >> 6) * NI * 1024;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      uint32_t off = voff[j];
+      if (guard && !keep(row_at(j, tid))) off = NOWHERE;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(dst + j * 1024), 16, (int)off, 0, 0, 0);
+    }
+  }
+};
+// every load of this wavefront has landed, then every wavefront's
+__device__ __forceinline__ void landed() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
+  asm volatile("" ::: "memory");
+  __syncthreads();
+  asm volatile("" ::: "memory");
 }
 
 __device__ __forceinline__ void store4(bf16* p, float a, float b, float c, float d) {
@@ -321,20 +345,25 @@ __device__ __forceinline__ void positions_range(const FormArgs& a, int b, int p0
   }
 }
 
-// Scores of 32 keys from k0 on (registers) for a lane's row: cap, distance, mask.
+// Scores of 32 keys from k0 on (registers) for a lane's row: cap, distance, mask.  What comes out times score_factor() is the
+// score in base 2; without cap and distance that leaves the factor to the exponential's own multiply-add.
+template <bool CAP>
+__device__ __forceinline__ float score_factor(const FormArgs& a, const Score& f) { return CAP || a.slopes ? 1.f : f.a; }
 template <bool CAP, bool DAMP>
 __device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int half, bool mask,
                                        f32x16_t& s, f32x16_t& damp) {
+  if constexpr (CAP) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float d = 1.f;
-    s[i] = score2<CAP>(f, s[i], d);
-    if constexpr (CAP && DAMP) damp[i] = d;
+    for (int i = 0; i < 16; ++i) {
+      float d = 1.f;
+      s[i] = score2<CAP>(f, s[i], d);
+      if constexpr (DAMP) damp[i] = d;
+    }
   }
   if (a.slopes) {
-    const float far = (float)(r.pos - k0 - 4 * half);
+    const float far = (float)(r.pos - k0 - 4 * half), c = CAP ? 1.f : f.a;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope2, fabsf(far - (float)acc_row(i)), s[i]);
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope2, fabsf(far - (float)acc_row(i)), c * s[i]);
   }
   if (mask) {
     const int lim = r.lim - k0 - 4 * half;
@@ -352,27 +381,62 @@ __device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const 
   }
 }
 
+// Tiles of keys and values, two of each: while one is worked on, the next one's loads are on their way.
+template <typename T, int D, int KT, int BUFS>
+struct KeyTiles {
+  static constexpr int TILE = KT * Tile<T, D>::ROWB, IDS = KT * 4, STAGE = 2 * TILE + IDS, LDS = BUFS * STAGE;
+  Loader<T, D, KT> kl, vl;
+  const T *k, *v;
+  const int32_t* docs;
+  int S;
+  long long ksr, vsr;
+  unsigned char* lds;
+  __device__ __forceinline__ void init(const FormArgs& a, int b, int hk, unsigned char* mem, int tid) {
+    k = head_ptr<T>(a.k, b, hk);
+    v = head_ptr<T>(a.v, b, hk);
+    docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
+    S = a.S;
+    ksr = a.k.sr;
+    vsr = a.v.sr;
+    lds = mem;
+    kl.init(tid, ksr * (int)sizeof(T), 1, 0, KT, a.w);
+    vl.init(tid, vsr * (int)sizeof(T), 1, 0, KT, a.w);
+  }
+  __device__ __forceinline__ unsigned char* keys(int i) const { return lds + (BUFS > 1 ? (i & 1) * STAGE : 0); }
+  __device__ __forceinline__ unsigned char* values(int i) const { return keys(i) + TILE; }
+  __device__ __forceinline__ const int* ids(int i) const { return reinterpret_cast<const int*>(keys(i) + 2 * TILE); }
+  // lo: least entry of the tile's documents
+  __device__ __forceinline__ void issue(int i, int k0, int lo, int tid) const {
+    const bool guard = k0 + KT > S || lo < 0;
+    auto keep = [&](int r) { return k0 + r < S && (docs == nullptr || docs[k0 + r] >= 0); };
+    kl.issue(k + k0 * ksr, keys(i), tid, guard, keep);
+    vl.issue(v + k0 * vsr, values(i), tid, guard, keep);
+    if (docs && tid < KT) {      // (entries past the last key are never looked at: positions limit first)
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(docs + k0), 0, 4 * (S - k0), 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(keys(i) + 2 * TILE + (tid >> 6) * 256), 4, 4 * tid, 0, 0, 0);
+    }
+  }
+};
+
 // ---- forward ----------------------------------------------------------------------------------------------------------
 // FEW = false: 128 rows, 32 per wavefront, tiles of 64 keys.  FEW = true: at most 32 rows (one query and its group, or a few);
 // the four wavefronts share them, each takes 32 keys of a tile of 128, and they join their results in LDS at the end.
 // Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
 template <typename T, int D, bool FEW>
 struct Fwd {
-  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 128;
-  static constexpr int TILE = KT * Tile<T, D>::ROWB;
+  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 128, BUFS = KT * Tile<T, D>::ROWB > 32768 ? 1 : 2;
+  using Keys = KeyTiles<T, D, KT, BUFS>;
   static constexpr int JOIN = FEW ? 4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 : 0;
-  static constexpr int LDS = 2 * TILE > JOIN ? 2 * TILE : JOIN;
+  static constexpr int LDS = Keys::LDS > JOIN ? Keys::LDS : JOIN;
 };
 
 template <typename T, int D, bool CAP, bool FEW>
-__global__ void __launch_bounds__(256) k_forms_fwd(FormArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_forms_fwd(FormArgs a) {
   using F = Fwd<T, D, FEW>;
+  constexpr int NK = FEW ? 1 : F::KT / 32;       // blocks of 32 keys of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int span_s[4][4];
-  __shared__ __attribute__((aligned(16))) int ids[F::KT];
-  unsigned char* const Ks = lds;
-  unsigned char* const Vs = lds + F::TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + F::ROWS - 1) / F::ROWS;
   int id = xcd_order(blockIdx.x, gridDim.x);
@@ -385,12 +449,12 @@ __global__ void __launch_bounds__(256) k_forms_fwd(FormArgs a) {
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const RowOf r = row_of(a, rt * F::ROWS + (FEW ? 0 : wave * 32) + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(r), gs = group_span(ws, span_s, wave, lane);
-  const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
   Frags<T, D> qf;
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
-  const T* kbase = head_ptr<T>(a.k, b, hk);
-  const T* vbase = head_ptr<T>(a.v, b, hk);
   const Score sc = make_score(a.scale, a.cap);
+  const float factor = score_factor<CAP>(a, sc);
+  typename F::Keys kv;
+  kv.init(a, b, hk, lds, tid);
 
   f32x16_t o[D / 32], unused;
 #pragma unroll
@@ -406,38 +470,53 @@ __global__ void __launch_bounds__(256) k_forms_fwd(FormArgs a) {
       take = tile_state(a, gs, t * F::KT, F::KT, lo, hi) != 0;
     }
     const int count = make_list(list, take, t, lo, hi, tid);
+    if (F::BUFS > 1 && count > 0) kv.issue(0, list.tile[0] * F::KT, list.lo[0], tid);
     for (int i = 0; i < count; ++i) {
       const int k0 = list.tile[i] * F::KT;
-      __syncthreads();
-      load_keys<T, D, F::KT>(Ks, kbase, a.k.sr, k0, a.S, a.w, docs, tid);
-      load_keys<T, D, F::KT>(Vs, vbase, a.v.sr, k0, a.S, a.w, docs, tid);
-      if (docs && tid < F::KT) ids[tid] = k0 + tid < a.S ? docs[k0 + tid] : -1;
-      __syncthreads();
+      if constexpr (F::BUFS > 1) {
+        landed();
+        if (i + 1 < count) kv.issue(i + 1, list.tile[i + 1] * F::KT, list.lo[i + 1], tid);
+      } else {
+        __syncthreads();
+        kv.issue(i, k0, list.lo[i], tid);
+        landed();
+      }
       const int state = tile_state(a, ws, k0, F::KT, list.lo[i], list.hi[i]);
       if (state == 0) continue;
-#pragma unroll 1
-      for (int kb = FEW ? wave : 0; kb < (FEW ? wave + 1 : F::KT / 32); ++kb) {
-        f32x16_t s = dot_rows<T, D>(Ks, 32 * kb, qf, lane);
-        scores<CAP, false>(a, sc, r, ids + 32 * kb, k0 + 32 * kb, half, state == 1, s, unused);
-        float top = s[0];
+      const int kb0 = FEW ? wave : 0;
+      f32x16_t s[NK];
 #pragma unroll
-        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
+      for (int kb = 0; kb < NK; ++kb) s[kb] = dot_rows<T, D>(kv.keys(i), 32 * (kb0 + kb), qf, lane);
+#pragma unroll
+      for (int kb = 0; kb < NK; ++kb)
+        scores<CAP, false>(a, sc, r, kv.ids(i) + 32 * (kb0 + kb), k0 + 32 * (kb0 + kb), half, state == 1, s[kb], unused);
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < NK; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[kb][j]);
+      top = factor * fmaxf(top, __shfl_xor(top, 32, 64));
+      // The exponentials' reference moves only when a score passes it by 2^8: any reference within that gives the same sums.
+      if (__any(top > m_run + 8.f)) {
         const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          s[j] = __builtin_amdgcn_exp2f(s[j] - m_new);
-          sum += s[j];
-        }
-        l_run = l_run * alpha + sum;
+        l_run *= alpha;
         m_run = m_new;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
           for (int j = 0; j < 16; ++j) o[db][j] *= alpha;
-        add_outer<T, D>(o, Vs, 32 * kb, s, lane);
       }
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < NK; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          s[kb][j] = __builtin_amdgcn_exp2f(fmaf(s[kb][j], factor, -m_run));
+          sum += s[kb][j];
+        }
+      l_run += sum;
+#pragma unroll
+      for (int kb = 0; kb < NK; ++kb) add_outer<T, D>(o, kv.values(i), 32 * (kb0 + kb), s[kb], lane);
     }
   }
   l_run += __shfl_xor(l_run, 32, 64);
@@ -536,15 +615,21 @@ __device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
   return s;
 }
 
+// bf16: the stored output is rounded, so sum_d dO O is not quite the delta that makes a row of p (dp - delta) add up to zero, and
+// in rows that look at few keys what is left is of the gradient's own size.  The kernel finds it, rest = sum p (dp - delta),
+// and takes it out: delta grows by rest, dQ loses rest * sum p damp k, for which those sums are formed beside dQ.
+template <typename T, int D>
+struct Bwd {
+  static constexpr int KT = 64;
+  using Keys = KeyTiles<T, D, KT, 2>;
+};
 template <typename T, int D, bool CAP>
-__global__ void __launch_bounds__(256) k_forms_bwd_q(FormArgs a) {
-  constexpr int KT = 64, TILE = KT * Tile<T, D>::ROWB;
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_forms_bwd_q(FormArgs a) {
+  constexpr int KT = Bwd<T, D>::KT;
+  constexpr bool MEND = sizeof(T) == 2;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int span_s[4][4];
-  __shared__ __attribute__((aligned(16))) int ids[KT];
-  unsigned char* const Ks = lds;
-  unsigned char* const Vs = lds + TILE;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + 127) / 128;
   int id = xcd_order(blockIdx.x, gridDim.x);
@@ -555,14 +640,14 @@ __global__ void __launch_bounds__(256) k_forms_bwd_q(FormArgs a) {
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const RowOf r = row_of(a, rt * 128 + wave * 32 + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(r), gs = group_span(ws, span_s, wave, lane);
-  const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
-  const T* kbase = head_ptr<T>(a.k, b, hk);
-  const T* vbase = head_ptr<T>(a.v, b, hk);
   const Score sc = make_score(a.scale, a.cap);
+  const float factor = score_factor<CAP>(a, sc);
+  typename Bwd<T, D>::Keys kv;
+  kv.init(a, b, hk, lds, tid);
 
   Frags<T, D> qf, gf;
   const size_t lrow = ((size_t)b * a.nh + r.head) * a.n + r.qi;
-  float l2 = INFINITY, delta = 0.f;
+  float l2 = INFINITY, delta = 0.f, rest = 0.f;
   if (r.live) {
     l2 = a.lse[lrow] * LOG2E;
     if (l2 == -INFINITY) l2 = INFINITY;       // sees no key: probabilities zero
@@ -575,12 +660,13 @@ __global__ void __launch_bounds__(256) k_forms_bwd_q(FormArgs a) {
 #pragma unroll
     for (int s = 0; s < Tile<T, D>::NS; ++s) delta += dot_chunk<T>(gf[s], of[s]);
     delta += __shfl_xor(delta, 32, 64);
-    if (r.in && half == 0) a.delta[lrow] = delta;
   }
 
-  f32x16_t dq[D / 32], damp;
+  f32x16_t dq[D / 32], pk[MEND ? D / 32 : 1], damp;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = zero16();
+#pragma unroll
+  for (int i = 0; MEND && i < D / 32; ++i) pk[i] = zero16();
   const int n_tiles = (a.S + KT - 1) / KT;
   for (int base = 0; base < n_tiles; base += LIST) {
     const int t = base + tid;
@@ -590,45 +676,61 @@ __global__ void __launch_bounds__(256) k_forms_bwd_q(FormArgs a) {
       take = tile_state(a, gs, t * KT, KT, lo, hi) != 0;
     }
     const int count = make_list(list, take, t, lo, hi, tid);
+    if (count > 0) kv.issue(0, list.tile[0] * KT, list.lo[0], tid);
     for (int i = 0; i < count; ++i) {
       const int k0 = list.tile[i] * KT;
-      __syncthreads();
-      load_keys<T, D, KT>(Ks, kbase, a.k.sr, k0, a.S, a.w, docs, tid);
-      load_keys<T, D, KT>(Vs, vbase, a.v.sr, k0, a.S, a.w, docs, tid);
-      if (docs && tid < KT) ids[tid] = k0 + tid < a.S ? docs[k0 + tid] : -1;
-      __syncthreads();
+      landed();
+      if (i + 1 < count) kv.issue(i + 1, list.tile[i + 1] * KT, list.lo[i + 1], tid);
       const int state = tile_state(a, ws, k0, KT, list.lo[i], list.hi[i]);
       if (state == 0) continue;
-#pragma unroll 1
+#pragma unroll
       for (int kb = 0; kb < KT / 32; ++kb) {
-        f32x16_t s = dot_rows<T, D>(Ks, 32 * kb, qf, lane);
-        f32x16_t dp = dot_rows<T, D>(Vs, 32 * kb, gf, lane);
-        scores<CAP, true>(a, sc, r, ids + 32 * kb, k0 + 32 * kb, half, state == 1, s, damp);
+        f32x16_t s = dot_rows<T, D>(kv.keys(i), 32 * kb, qf, lane);
+        f32x16_t dp = dot_rows<T, D>(kv.values(i), 32 * kb, gf, lane);
+        scores<CAP, true>(a, sc, r, kv.ids(i) + 32 * kb, k0 + 32 * kb, half, state == 1, s, damp);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          s[j] = __builtin_amdgcn_exp2f(s[j] - l2) * (dp[j] - delta);
-          if constexpr (CAP) s[j] *= damp[j];
+          float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
+          if constexpr (MEND) rest += ds;
+          if constexpr (CAP) {
+            ds *= damp[j];
+            p *= damp[j];
+          }
+          s[j] = p;
+          dp[j] = ds;
         }
-        add_outer<T, D>(dq, Ks, 32 * kb, s, lane);
+        add_outer<T, D>(dq, kv.keys(i), 32 * kb, dp, lane);
+        if constexpr (MEND) add_outer<T, D>(pk, kv.keys(i), 32 * kb, s, lane);
       }
     }
   }
-  if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
+  if constexpr (MEND) {
+    rest += __shfl_xor(rest, 32, 64);
+    delta += rest;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
+  }
+  if (!r.in) return;
+  if (half == 0) a.delta[lrow] = delta;
+  store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
 }
 
 // ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
-// 128 keys, 32 per wavefront, over tiles of 64 rows of the group's heads.
+// 128 keys, 32 per wavefront, over tiles of the 64 / G queries whose rows fit 64 (G: heads of the group).
+struct RowMeta {
+  float l2[64], delta[64], slope[64];
+  int lim[64], id[64], pos[64];
+};
 template <typename T, int D, bool CAP>
-__global__ void __launch_bounds__(256) k_forms_bwd_kv(FormArgs a) {
-  constexpr int RT = 64, TILE = RT * Tile<T, D>::ROWB, CPR = Tile<T, D>::CPR;
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
+  constexpr int RT = 64, TILE = RT * Tile<T, D>::ROWB;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ TileList list;
-  __shared__ __attribute__((aligned(16))) float l2_s[RT], delta_s[RT], slope_s[RT];
-  __shared__ __attribute__((aligned(16))) int lim_s[RT], id_s[RT], pos_s[RT];
-  unsigned char* const Qs = lds;
-  unsigned char* const Gs = lds + TILE;
+  __shared__ __attribute__((aligned(16))) RowMeta meta[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int G = a.nh / a.nkv, rows = a.n * G, n_kt = (a.S + 127) / 128, first = a.S - a.n;
+  const int G = a.nh / a.nkv, QT = RT / G, used = QT * G, n_kt = (a.S + 127) / 128, first = a.S - a.n;
   int id = xcd_order(blockIdx.x, gridDim.x);
   const int kt = id % n_kt;
   id /= n_kt;
@@ -651,83 +753,98 @@ __global__ void __launch_bounds__(256) k_forms_bwd_kv(FormArgs a) {
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
 
-  const int n_tiles = (rows + RT - 1) / RT;
+  Loader<T, D, RT> ql, gl;
+  ql.init(tid, a.q.sr * (int)sizeof(T), G, a.q.sh * (int)sizeof(T), used, a.w);
+  gl.init(tid, a.g.sr * (int)sizeof(T), G, a.g.sh * (int)sizeof(T), used, a.w);
+  const T* qbase = head_ptr<T>(a.q, b, hk * G);
+  const T* gbase = head_ptr<T>(a.g, b, hk * G);
+  auto tiles = [&](int i) { return lds + (i & 1) * 2 * TILE; };
+  // queries q0 .. q0 + QT - 1 of all heads of the group; what the mask needs of a row waits in the registers of wavefront 0
+  RowOf mr;
+  float ml2 = 0.f, mdelta = 0.f;
+  auto issue = [&](int i, int q0, int lo) {
+    if (tid < RT) {
+      const int R = tid < used ? q0 * G + tid : 0x7fffffff;
+      mr = row_of(a, R, b, hk, prefix);
+      const size_t lrow = ((size_t)b * a.nh + mr.head) * a.n + mr.qi;
+      ml2 = mr.live ? a.lse[lrow] : -INFINITY;
+      mdelta = mr.live ? a.delta[lrow] : 0.f;
+    }
+    const bool guard = q0 + QT > a.n || lo < 0;
+    auto keep = [&](int r) { return q0 + r / G < a.n && (docs == nullptr || docs[first + q0 + r / G] >= 0); };
+    ql.issue(qbase + q0 * a.q.sr, tiles(i), tid, guard, keep);
+    gl.issue(gbase + q0 * a.g.sr, tiles(i) + TILE, tid, guard, keep);
+  };
+  auto commit = [&](int i) {
+    if (tid >= RT) return;
+    RowMeta& m = meta[i & 1];
+    m.l2[tid] = ml2 == -INFINITY ? INFINITY : ml2 * LOG2E;     // rows that see nothing: probabilities zero
+    m.delta[tid] = mdelta;
+    m.slope[tid] = mr.slope2;
+    m.lim[tid] = mr.lim;
+    m.id[tid] = mr.id;
+    m.pos[tid] = mr.pos;
+  };
+
+  const int n_tiles = (a.n + QT - 1) / QT;
   for (int base = 0; base < n_tiles; base += LIST) {
     const int t = base + tid;
     int lo = 0, hi = 0, take = 0;
     if (t < n_tiles) {
-      const int p0 = first + t * RT / G, p1 = first + min(rows - 1, t * RT + RT - 1) / G;
+      const int p0 = first + t * QT, p1 = first + min(a.n, t * QT + QT) - 1;
       positions_range(a, b, p0, p1, lo, hi);
       take = kt * 128 < key_limit(a, p1, prefix) && (!docs || (hi >= 0 && khi >= 0 && lo <= khi && hi >= klo));
     }
     const int count = make_list(list, take, t, lo, hi, tid);
+    if (count > 0) {
+      issue(0, list.tile[0] * QT, list.lo[0]);
+      commit(0);
+    }
     for (int i = 0; i < count; ++i) {
-      const int R0 = list.tile[i] * RT, p0 = first + R0 / G, p1 = first + min(rows - 1, R0 + RT - 1) / G;
+      const int q0 = list.tile[i] * QT, p0 = first + q0, p1 = first + min(a.n, q0 + QT) - 1;
       const int lo_t = list.lo[i], hi_t = list.hi[i];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < RT * CPR / 256; ++j) {
-        const int idx = tid + 256 * j, row = idx / CPR, c = idx % CPR, R = R0 + row;
-        u32x4_t q = u32x4_t{0, 0, 0, 0}, g = q;
-        if (R < rows && c * Tile<T, D>::CH < a.w) {
-          const int qi = R / G, head = hk * G + R % G;
-          if (!docs || docs[first + qi] >= 0) {
-            q = *reinterpret_cast<const u32x4_t*>(head_ptr<T>(a.q, b, head) + (long long)qi * a.q.sr + c * Tile<T, D>::CH);
-            g = *reinterpret_cast<const u32x4_t*>(head_ptr<T>(a.g, b, head) + (long long)qi * a.g.sr + c * Tile<T, D>::CH);
-          }
-        }
-        *Tile<T, D>::at(Qs, row, c) = q;
-        *Tile<T, D>::at(Gs, row, c) = g;
-      }
-      if (tid < RT) {
-        const RowOf r = row_of(a, R0 + tid, b, hk, prefix);
-        const size_t lrow = ((size_t)b * a.nh + r.head) * a.n + r.qi;
-        const float l2 = r.live ? a.lse[lrow] * LOG2E : INFINITY;
-        l2_s[tid] = l2 == -INFINITY ? INFINITY : l2;
-        delta_s[tid] = r.live ? a.delta[lrow] : 0.f;
-        slope_s[tid] = r.slope2;
-        lim_s[tid] = r.lim;
-        id_s[tid] = r.id;
-        pos_s[tid] = r.pos;
-      }
-      __syncthreads();
-      if (kw >= key_limit(a, p1, prefix) || kid_hi < 0) continue;
-      if (docs && (hi_t < kid_lo || lo_t > kid_hi)) continue;
+      landed();
+      if (i + 1 < count) issue(i + 1, list.tile[i + 1] * QT, list.lo[i + 1]);
+      const RowMeta& m = meta[i & 1];
+      const bool hidden = kw >= key_limit(a, p1, prefix) || kid_hi < 0 || (docs && (hi_t < kid_lo || lo_t > kid_hi));
       const bool mask = kw + 32 > key_limit(a, p0, prefix) || (docs && !(lo_t == hi_t && lo_t == kid_lo && lo_t == kid_hi));
+      if (!hidden) {
 #pragma unroll 1
-      for (int rb = 0; rb < RT / 32; ++rb) {
-        f32x16_t s = dot_rows<T, D>(Qs, 32 * rb, kf, lane);
-        f32x16_t dp = dot_rows<T, D>(Gs, 32 * rb, vf, lane);
+        for (int rb = 0; rb < RT / 32; ++rb) {
+          f32x16_t s = dot_rows<T, D>(tiles(i), 32 * rb, kf, lane);
+          f32x16_t dp = dot_rows<T, D>(tiles(i) + TILE, 32 * rb, vf, lane);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int at = 32 * rb + 8 * g + 4 * half;
-          const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(l2_s + at), dl = *reinterpret_cast<const f32x4_t*>(delta_s + at);
-          f32x4_t sl = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          int4 ps = make_int4(0, 0, 0, 0);
-          if (a.slopes) {
-            sl = *reinterpret_cast<const f32x4_t*>(slope_s + at);
-            ps = *reinterpret_cast<const int4*>(pos_s + at);
-          }
-          const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
-          int4 lm = make_int4(0, 0, 0, 0), qi = lm;
-          if (mask) {
-            lm = *reinterpret_cast<const int4*>(lim_s + at);
-            qi = *reinterpret_cast<const int4*>(id_s + at);
-          }
-          const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
+          for (int g = 0; g < 4; ++g) {
+            const int at = 32 * rb + 8 * g + 4 * half;
+            const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at);
+            float x[4], d[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float d = 1.f, x = score2<CAP>(sc, s[4 * g + j], d);
-            if (a.slopes) x = fmaf(-sl[j], fabsf((float)(pos[j] - key)), x);
-            if (mask) x = key < lim[j] && (!docs || qid[j] == kid) ? x : -INFINITY;
-            const float p = __builtin_amdgcn_exp2f(x - l2[j]);
-            s[4 * g + j] = p;
-            dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * d;
+            for (int j = 0; j < 4; ++j) x[j] = score2<CAP>(sc, s[4 * g + j], d[j]);
+            if (a.slopes) {
+              const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at);
+              const int4 ps = *reinterpret_cast<const int4*>(m.pos + at);
+              const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), x[j]);
+            }
+            if (mask) {
+              const int4 lm = *reinterpret_cast<const int4*>(m.lim + at), qi = *reinterpret_cast<const int4*>(m.id + at);
+              const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x[j] = key < lim[j] && (!docs || qid[j] == kid) ? x[j] : -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float p = __builtin_amdgcn_exp2f(x[j] - l2[j]);
+              s[4 * g + j] = p;
+              dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * d[j];
+            }
           }
+          add_outer<T, D>(dv, tiles(i) + TILE, 32 * rb, s, lane);
+          add_outer<T, D>(dk, tiles(i), 32 * rb, dp, lane);
         }
-        add_outer<T, D>(dv, Gs, 32 * rb, s, lane);
-        add_outer<T, D>(dk, Qs, 32 * rb, dp, lane);
       }
+      if (i + 1 < count) commit(i + 1);
     }
   }
   if (!in) return;
@@ -766,10 +883,9 @@ template <typename T, int D, bool CAP>
 hipError_t bwd_w(const FormArgs& a, hipStream_t s) {
   const int rows = a.n * (a.nh / a.nkv);
   const size_t heads = (size_t)a.B * a.nkv;
-  constexpr int LDS = 2 * 64 * Tile<T, D>::ROWB;
-  const hipError_t e = launch<k_forms_bwd_q<T, D, CAP>>(heads * ((rows + 127) / 128), LDS, a, s);
+  const hipError_t e = launch<k_forms_bwd_q<T, D, CAP>>(heads * ((rows + 127) / 128), Bwd<T, D>::Keys::LDS, a, s);
   if (e != hipSuccess) return e;
-  return launch<k_forms_bwd_kv<T, D, CAP>>(heads * ((a.S + 127) / 128), LDS, a, s);
+  return launch<k_forms_bwd_kv<T, D, CAP>>(heads * ((a.S + 127) / 128), 4 * 64 * Tile<T, D>::ROWB, a, s);
 }
 template <typename T>
 hipError_t fwd_t(const FormArgs& a, hipStream_t s) {

@@ -180,6 +180,7 @@ static int attention_sizes(const char* who, int precision, int batch, int querie
   if (precision != 0 && precision != 1) return fail(MSLT_ERR_ARG, "%s: precision must be 0 or 1", who);
   if (batch < 1 || queries < 1 || keys < queries || heads < 1 || kv_heads < 1 || heads % kv_heads || width < 1)
     return fail(MSLT_ERR_ARG, "%s: needs 1 <= queries <= keys and heads a multiple of kv_heads", who);
+  if (heads / kv_heads > 64) return fail(MSLT_ERR_ARG, "%s: more than 64 heads to a kv head", who);
   if (width > 128 || width % (precision ? 8 : 4)) return fail(MSLT_ERR_ARG, "%s: width must be a multiple of 16 bytes, at most 128", who);
   // positions as fp32 and tiles as a grid
   if (keys > (1 << 24) || (long long)batch * heads > (1 << 20) || (long long)batch * heads * keys > (1ll << 34) ||
@@ -229,6 +230,9 @@ static int attention_args(const char* who, int precision, int batch, int queries
   HEADS_OK(q, queries, heads, true, false);
   HEADS_OK(k, keys, kv_heads, true, false);
   HEADS_OK(v, keys, kv_heads, true, false);
+  // a tile is addressed by 32-bit offsets from its first row
+  if (keys > 1 && (k->row_stride > (1 << 22) || v->row_stride > (1 << 22)))
+    return fail(MSLT_ERR_ARG, "%s: a row stride of k or v above 2^22 elements", who);
   if (!f) return fail(MSLT_ERR_ARG, "%s: form is null", who);
   if (!(f->scale > 0.f) || !std::isfinite(f->scale)) return fail(MSLT_ERR_ARG, "%s: scale must be above 0", who);
   if (!(f->cap >= 0.f) || !std::isfinite(f->cap)) return fail(MSLT_ERR_ARG, "%s: cap must be 0 or above", who);
@@ -275,6 +279,11 @@ extern "C" int mslt_attention_backward(void* hip_stream, int precision, int batc
   if (rc) return rc;
   HEADS_OK(out, queries, heads, true, false);
   HEADS_OK(grad_out, queries, heads, true, false);
+  for (const mslt_heads* x : {q, grad_out}) {
+    const int group = heads / kv_heads;
+    if ((queries > 1 && x->row_stride > (1 << 22)) || (group > 1 && x->head_stride > (1ll << 28) / group))
+      return fail(MSLT_ERR_ARG, "%s: q or grad_out: a row stride above 2^22 elements, or heads of a group 2^28 elements apart", who);
+  }
   HEADS_OK(dq, queries, heads, true, true);
   HEADS_OK(dk, keys, kv_heads, true, true);
   HEADS_OK(dv, keys, kv_heads, true, true);
