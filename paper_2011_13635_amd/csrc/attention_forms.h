@@ -88,13 +88,50 @@ __device__ __forceinline__ f32x16_t mma(u32x4_t a, u32x4_t b, f32x16_t acc) {
     return acc;
   }
 }
+// LDS addresses.  A lane's address in a tile is its lane part plus the tile's, and a constant of the step over it (exclusive or,
+// where the step changes the chunk; a tile's address is a multiple of its row): one instruction for a read, and two registers
+// of addresses in all.  Kept in a register each, the addresses of all steps cost the accumulators' room.
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t addr) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) V*>((uintptr_t)addr);
+}
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+constexpr int TILE_ALIGN = 512;      // of every tile in LDS: the longest row
+template <typename T, int D>
+struct Lane {
+  uint32_t rows, cols;     // parts of a read by rows (first products), and of one by columns (second products)
+  __device__ __forceinline__ explicit Lane(int lane) {
+    using L = Tile<T, D>;
+    const int n = lane & 31, half = lane >> 5;
+    rows = n * L::ROWB + 16 * (half ^ L::swz(n));
+    if constexpr (sizeof(T) == 2) {
+      // sixteen lanes fetch four consecutive rows of sixteen d and receive four rows of one d each
+      const int j = lane & 15, blk = (lane >> 4) & 1, row = 4 * half + (j >> 2);
+      cols = row * L::ROWB + 16 * ((2 * blk + ((j & 3) >> 1)) ^ L::swz(row)) + 8 * (j & 1);
+    } else {
+      cols = 4 * half * L::ROWB + 16 * ((n >> 2) ^ (half << 3)) + 4 * (n & 3);
+    }
+  }
+};
 // [32 tile rows from row0] x [fragment rows]: lane = fragment row, registers = tile rows
 template <typename T, int D>
-__device__ __forceinline__ f32x16_t dot_rows(unsigned char* tile, int row0, const Frags<T, D>& f, int lane) {
+__device__ __forceinline__ f32x16_t dot_rows(uint32_t tile, int row0, const Frags<T, D>& f, const Lane<T, D>& l) {
   f32x16_t acc = zero16();
-  const int row = row0 + (lane & 31), half = lane >> 5;
+  const uint32_t at = tile + l.rows;
 #pragma unroll
-  for (int s = 0; s < Tile<T, D>::NS; ++s) acc = mma<T>(*Tile<T, D>::at(tile, row, 2 * s + half), f[s], acc);
+  for (int s = 0; s < Tile<T, D>::NS; ++s) acc = mma<T>(lds_read<u32x4_t>((at ^ (32 * s)) + row0 * Tile<T, D>::ROWB), f[s], acc);
+  return acc;
+}
+// the same with the fragments read out of a second tile's rows
+template <typename T, int D>
+__device__ __forceinline__ f32x16_t dot_tiles(uint32_t tile, int row0, uint32_t other, const Lane<T, D>& l) {
+  f32x16_t acc = zero16();
+  const uint32_t at = tile + l.rows, to = other + l.rows;
+#pragma unroll
+  for (int s = 0; s < Tile<T, D>::NS; ++s)
+    acc = mma<T>(lds_read<u32x4_t>((at ^ (32 * s)) + row0 * Tile<T, D>::ROWB), lds_read<u32x4_t>(to ^ (32 * s)), acc);
   return acc;
 }
 // registers 8c .. 8c+7 as a B operand
@@ -104,41 +141,56 @@ __device__ __forceinline__ bf16x8_t pack_frag(const f32x16_t& p, int c) {
   for (int i = 0; i < 4; ++i) u[i] = pack_bf16x2(p[8 * c + 2 * i], p[8 * c + 2 * i + 1]);
   return __builtin_bit_cast(bf16x8_t, u);
 }
+// bf16: rows row0 + 16c + 8i + 4half + 0 .. 3, i = 0, 1, of a tile at d = 32 db + lane % 32
+template <int D>
+__device__ __forceinline__ bf16x8_t frag_transposed(uint32_t tile, int row0, int c, int db, const Lane<bf16, D>& l) {
+  const uint32_t at = tile + l.cols;
+  s16x4_t v[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)((at ^ (64 * db + 32 * i)) + (row0 + 16 * c + 8 * i) * Tile<bf16, D>::ROWB));
+  struct { s16x4_t lo, hi; } w{v[0], v[1]};
+  return __builtin_bit_cast(bf16x8_t, w);
+}
 // acc[d, lane's column] += sum over 32 tile rows from row0 of tile[row][d] * p[row, column].  bf16: p is rounded to bf16
-// here, the one rounding between the two products (the sum of a row is taken before it); a term is then off by 2^-9 of
-// itself, as the operands of the first product already are.
+// here, the one rounding between the two products (the sum of a row is taken before it); a term is then off by half a step,
+// 2^-8 of itself, as the operands of the first product already are.
+template <int D>
+__device__ __forceinline__ void add_packed(f32x16_t (&acc)[D / 32], uint32_t tile, int row0, const bf16x8_t (&f)[2], const Lane<bf16, D>& l) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+      acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_transposed<D>(tile, row0, c, db, l), f[c], acc[db], 0, 0, 0);
+}
 template <typename T, int D>
-__device__ __forceinline__ void add_outer(f32x16_t (&acc)[D / 32], unsigned char* tile, int row0, const f32x16_t& p, int lane) {
-  const int half = lane >> 5;
+__device__ __forceinline__ void add_outer(f32x16_t (&acc)[D / 32], uint32_t tile, int row0, const f32x16_t& p, const Lane<T, D>& l) {
   if constexpr (sizeof(T) == 2) {
-    const int j = lane & 15, blk = (lane >> 4) & 1;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const bf16x8_t f = pack_frag(p, c);
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        s16x4_t v[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          // sixteen lanes fetch four consecutive rows of sixteen d and receive four rows of one d each
-          const int row = row0 + 16 * c + 8 * i + 4 * half + (j >> 2), d = 32 * db + 16 * blk + 4 * (j & 3);
-          unsigned char* src = tile + row * Tile<T, D>::ROWB + 16 * ((d >> 3) ^ Tile<T, D>::swz(row)) + 2 * (d & 7);
-          v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)src);
-        }
-        struct { s16x4_t lo, hi; } w{v[0], v[1]};
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, w), f, acc[db], 0, 0, 0);
-      }
-    }
+    const bf16x8_t f[2] = {pack_frag(p, 0), pack_frag(p, 1)};
+    add_packed<D>(acc, tile, row0, f, l);
   } else {
+    const uint32_t at = tile + l.cols;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int row = row0 + acc_row(r) + 4 * half;
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        const int d = 32 * db + (lane & 31);
-        const float x = *reinterpret_cast<const float*>(tile + row * Tile<T, D>::ROWB + 16 * ((d >> 2) ^ Tile<T, D>::swz(row)) + 4 * (d & 3));
+        const float x = lds_read<float>((at ^ (16 * (8 * db + (r & 3) + ((r >> 2) & 1) * 4))) + (row0 + acc_row(r)) * Tile<T, D>::ROWB);
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[r], acc[db], 0, 0, 0);
       }
+  }
+}
+// two such products of the same tile (bf16)
+template <typename T, int D>
+__device__ __forceinline__ void add_outer2(f32x16_t (&x)[D / 32], f32x16_t (&y)[D / 32], uint32_t tile, int row0, const f32x16_t& p,
+                                           const f32x16_t& q, const Lane<T, D>& l) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const bf16x8_t f = pack_frag(p, c), g = pack_frag(q, c);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const bf16x8_t t = frag_transposed<D>(tile, row0, c, db, l);
+      x[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t, f, x[db], 0, 0, 0);
+      y[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t, g, y[db], 0, 0, 0);
     }
   }
 }
@@ -161,22 +213,39 @@ __device__ __forceinline__ Score make_score(float scale, float cap) {
 
 __device__ __forceinline__ const int2* range_row(const FormArgs& a, int b) { return a.ranges + (size_t)b * ((a.S + 63) / 64); }
 
-// The workgroups of one kv head run one after the other on one XCD, whose L2 then holds its keys and values.
-__device__ __forceinline__ int xcd_order(int id, int total) {
-  const int q = total >> 3, r = total & 7, x = id & 7;
-  return x * q + min(x, r) + (id >> 3);
+// Which tile of which kv head a workgroup takes.  Workgroups go round the eight XCDs; the tiles of one kv head are given to one
+// XCD, or to 8 / heads of them when there are fewer heads, so that its keys and values stay in few L2s.  uneven (causal): tiles
+// differ in work and come longest first; heads that do not divide so are then dealt out tile by tile, as an XCD with the
+// first tiles of a head only would finish last (1x8192, 4 kv heads: 492 us when cut into eight runs, TODO us so).
+__device__ __forceinline__ void tile_order(int id, int heads, int tiles, bool uneven, int& head, int& tile) {
+  const int x = id & 7, i = id >> 3;
+  if (heads % 8 == 0) {
+    head = x + 8 * (i / tiles);
+    tile = i % tiles;
+  } else if (8 % heads == 0 && tiles % (8 / heads) == 0) {
+    const int share = 8 / heads;
+    head = x / share;
+    tile = i * share + x % share;
+  } else if (uneven) {
+    head = id % heads;
+    tile = id / heads;
+  } else {
+    const int total = heads * tiles, q = total >> 3, r = total & 7, at = x * q + min(x, r) + i;
+    head = at / tiles;
+    tile = at % tiles;
+  }
 }
 
 struct TileList {
   int tile[LIST], lo[LIST], hi[LIST];
   int count[4];
 };
-// Appends the tiles of the threads that ask for it; returns how many there are.  Called by the whole workgroup of 256.
+// Lists the tiles of the first 256 threads that ask for it; returns how many there are.  Called by the whole workgroup.
 __device__ __forceinline__ int make_list(TileList& l, bool take, int tile, int lo, int hi, int tid) {
   const unsigned long long m = __ballot(take);
   const int wave = tid >> 6, lane = tid & 63;
   __syncthreads();            // the list before this one has been read
-  if (lane == 0) l.count[wave] = __popcll(m);
+  if (lane == 0 && wave < 4) l.count[wave] = __popcll(m);
   __syncthreads();
   int at = __popcll(m & ((1ull << lane) - 1ull)), n = 0;
 #pragma unroll
@@ -215,11 +284,31 @@ __device__ __forceinline__ void load_frags(Frags<T, D>& f, const T* row, int hal
 // Rows go from memory into a tile directly, 64 lanes x 16 bytes an instruction to 1024 consecutive bytes of LDS; which piece a
 // lane fetches is free, which is where the swizzle lives.  A lane whose piece is none of the operand's (a row past the end, a
 // row of padding, elements past the width) fetches beyond the buffer's end, which writes zeros.
+// The load is written out: behind the builtin the compiler lets every transposed read wait for all loads on their way, as it
+// cannot tell the tiles apart (1x8192, 16 heads of 128: 367 us, TODO us without).  It returns nothing to a register; wait_loads()
+// and a barrier stand between it and the reads.
 constexpr uint32_t NOWHERE = 0x80000000u;
-typedef __attribute__((address_space(3))) void lds_void_t;
-template <typename T, int D, int ROWS>
+struct Source {
+  u32x4_t rsrc;
+  __device__ __forceinline__ Source(const void* base, uint32_t bytes) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base);
+    rsrc = u32x4_t{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) & 0xffffu,
+                   (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+    // a memory instruction may read a scalar register five wait states after a vector instruction wrote it; inside a written
+    // out load the compiler does not see to that
+    asm volatile("s_nop 4" : "+s"(rsrc));
+  }
+  // 16 (4) bytes a lane from its offset to LDS address `to` + 16 (4) * lane; `to` the same for the wavefront
+  __device__ __forceinline__ void load16(uint32_t off, uint32_t to) const {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(off), "s"(rsrc) : "memory");
+  }
+  __device__ __forceinline__ void load4(uint32_t off, uint32_t to) const {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(off), "s"(rsrc) : "memory");
+  }
+};
+template <typename T, int D, int ROWS, int NW>
 struct Loader {
-  static constexpr int CPR = Tile<T, D>::CPR, NI = ROWS * CPR / 256;
+  static constexpr int CPR = Tile<T, D>::CPR, NI = ROWS * CPR / (64 * NW);
   uint32_t voff[NI];
   static __device__ __forceinline__ int row_at(int j, int tid) { return (64 * ((tid >> 6) * NI + j) + (tid & 63)) / CPR; }
   // row r of the tile lies (r / group) * row_bytes + (r % group) * head_bytes behind the base; rows from `used` on are none
@@ -232,23 +321,38 @@ struct Loader {
     }
   }
   template <typename Keep>
-  __device__ __forceinline__ void issue(const T* base, unsigned char* tile, int tid, bool guard, Keep keep) const {
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, 0x7fffffff, 0x00020000);
-    unsigned char* const dst = tile + (tid >> 6) * NI * 1024;
+  __device__ __forceinline__ void issue(const T* base, uint32_t tile, int tid, bool guard, Keep keep) const {
+    const Source src(base, 0x7fffffffu);
+    const uint32_t dst = __builtin_amdgcn_readfirstlane((int)(tile + (tid >> 6) * NI * 1024));
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       uint32_t off = voff[j];
       if (guard && !keep(row_at(j, tid))) off = NOWHERE;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(dst + j * 1024), 16, (int)off, 0, 0, 0);
+      src.load16(off, dst + j * 1024);
     }
   }
 };
-// every load of this wavefront has landed, then every wavefront's
-__device__ __forceinline__ void landed() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
+// At most `later` stages of PER loads of this wavefront are still on their way.
+template <int PER, int STAGES>
+__device__ __forceinline__ void wait_loads(int later) {
+  static_assert(STAGES <= 4 && (STAGES - 2) * PER < 64, "the counter's range");
+  constexpr auto vmcnt = [](int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); };
+  if (STAGES > 3 && later >= 2) __builtin_amdgcn_s_waitcnt(vmcnt(2 * PER));
+  else if (STAGES > 2 && later >= 1) __builtin_amdgcn_s_waitcnt(vmcnt(PER));
+  else __builtin_amdgcn_s_waitcnt(vmcnt(0));
+}
+__device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
-  __syncthreads();
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
   asm volatile("" ::: "memory");
+}
+// The loads of the stage at hand have landed, this wavefront's and then every one's.
+template <int PER, int STAGES>
+__device__ __forceinline__ void landed(int later) {
+  wait_loads<PER, STAGES>(later);
+  meet();
 }
 
 __device__ __forceinline__ void store4(bf16* p, float a, float b, float c, float d) {
@@ -307,7 +411,8 @@ __device__ __forceinline__ Span wave_span(const RowOf& r) {
   constexpr int BIG = 0x7fffffff;
   return Span{wave_min_i(r.live ? r.lim : BIG), wave_max_i(r.lim), wave_min_i(r.live ? r.id : BIG), wave_max_i(r.live ? r.id : -1)};
 }
-__device__ __forceinline__ Span group_span(const Span& w, int (&shared)[4][4], int wave, int lane) {
+template <int NW>
+__device__ __forceinline__ Span group_span(const Span& w, int (&shared)[NW][4], int wave, int lane) {
   if (lane == 0) {
     shared[wave][0] = w.lim_lo;
     shared[wave][1] = w.lim_hi;
@@ -317,7 +422,7 @@ __device__ __forceinline__ Span group_span(const Span& w, int (&shared)[4][4], i
   __syncthreads();
   Span s = w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < NW; ++i) {
     s.lim_lo = min(s.lim_lo, shared[i][0]);
     s.lim_hi = max(s.lim_hi, shared[i][1]);
     s.id_lo = min(s.id_lo, shared[i][2]);
@@ -345,13 +450,12 @@ __device__ __forceinline__ void positions_range(const FormArgs& a, int b, int p0
   }
 }
 
-// Scores of 32 keys from k0 on (registers) for a lane's row: cap, distance, mask.  What comes out times score_factor() is the
-// score in base 2; without cap and distance that leaves the factor to the exponential's own multiply-add.
-template <bool CAP>
-__device__ __forceinline__ float score_factor(const FormArgs& a, const Score& f) { return CAP || a.slopes ? 1.f : f.a; }
-template <bool CAP, bool DAMP>
-__device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int half, bool mask,
-                                       f32x16_t& s, f32x16_t& damp) {
+// Scores of 32 keys from k0 on (registers) for a lane's row: cap and distance, then the mask.  What comes out times
+// score_factor() is the score in base 2; without cap and distance that leaves the factor to the exponential's own multiply-add.
+template <bool CAP, bool SLOPES>
+__device__ __forceinline__ float score_factor(const Score& f) { return CAP || SLOPES ? 1.f : f.a; }
+template <bool CAP, bool SLOPES, bool DAMP>
+__device__ __forceinline__ void open_scores(const Score& f, const RowOf& r, int k0, int half, f32x16_t& s, f32x16_t& damp) {
   if constexpr (CAP) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -360,32 +464,42 @@ __device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const 
       if constexpr (DAMP) damp[i] = d;
     }
   }
-  if (a.slopes) {
+  if constexpr (SLOPES) {
     const float far = (float)(r.pos - k0 - 4 * half), c = CAP ? 1.f : f.a;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope2, fabsf(far - (float)acc_row(i)), c * s[i]);
   }
-  if (mask) {
-    const int lim = r.lim - k0 - 4 * half;
+}
+// the keys that the row does not see get -infinity
+__device__ __forceinline__ void hide(const FormArgs& a, const RowOf& r, const int* ids, int k0, int half, f32x16_t& s) {
+  const int lim = r.lim - k0 - 4 * half;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = acc_row(i) < lim ? s[i] : -INFINITY;
-    if (a.docs) {
+  for (int i = 0; i < 16; ++i) s[i] = acc_row(i) < lim ? s[i] : -INFINITY;
+  if (a.docs) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int4 v = *reinterpret_cast<const int4*>(ids + 8 * g + 4 * half);
-        const int id[4] = {v.x, v.y, v.z, v.w};
+    for (int g = 0; g < 4; ++g) {
+      const int4 v = *reinterpret_cast<const int4*>(ids + 8 * g + 4 * half);
+      const int id[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[4 * g + j] = id[j] == r.id ? s[4 * g + j] : -INFINITY;
-      }
+      for (int j = 0; j < 4; ++j) s[4 * g + j] = id[j] == r.id ? s[4 * g + j] : -INFINITY;
     }
   }
 }
+template <bool CAP, bool SLOPES, bool DAMP>
+__device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int half, bool mask,
+                                       f32x16_t& s, f32x16_t& damp) {
+  open_scores<CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
+  if (mask) hide(a, r, ids, k0, half, s);
+}
 
-// Tiles of keys and values, two of each: while one is worked on, the next one's loads are on their way.
-template <typename T, int D, int KT, int BUFS>
+// Tiles of keys and values in STAGES stages: while one is worked on, the loads of the next ones are on their way.
+template <typename T, int D, int KT, int STAGES, int NW>
 struct KeyTiles {
-  static constexpr int TILE = KT * Tile<T, D>::ROWB, IDS = KT * 4, STAGE = 2 * TILE + IDS, LDS = BUFS * STAGE;
-  Loader<T, D, KT> kl, vl;
+  static constexpr int TILE = KT * Tile<T, D>::ROWB, IDS = 512, STAGE = 2 * TILE + IDS, LDS = STAGES * STAGE;
+  static_assert(KT * 4 <= IDS && TILE % TILE_ALIGN == 0, "tiles start on whole rows");
+  using Load = Loader<T, D, KT, NW>;
+  static constexpr int PER = 2 * Load::NI;      // loads of a wavefront for a stage (a wavefront with entries of documents: one more)
+  Load kl, vl;
   const T *k, *v;
   const int32_t* docs;
   int S;
@@ -402,57 +516,88 @@ struct KeyTiles {
     kl.init(tid, ksr * (int)sizeof(T), 1, 0, KT, a.w);
     vl.init(tid, vsr * (int)sizeof(T), 1, 0, KT, a.w);
   }
-  __device__ __forceinline__ unsigned char* keys(int i) const { return lds + (BUFS > 1 ? (i & 1) * STAGE : 0); }
-  __device__ __forceinline__ unsigned char* values(int i) const { return keys(i) + TILE; }
-  __device__ __forceinline__ const int* ids(int i) const { return reinterpret_cast<const int*>(keys(i) + 2 * TILE); }
-  // lo: least entry of the tile's documents
-  __device__ __forceinline__ void issue(int i, int k0, int lo, int tid) const {
-    const bool guard = k0 + KT > S || lo < 0;
+  __device__ __forceinline__ uint32_t keys(int i) const { return lds_addr(lds) + (i & (STAGES - 1)) * STAGE; }
+  __device__ __forceinline__ uint32_t values(int i) const { return keys(i) + TILE; }
+  __device__ __forceinline__ const int* ids(int i) const { return reinterpret_cast<const int*>(lds + (i & (STAGES - 1)) * STAGE + 2 * TILE); }
+  __device__ __forceinline__ void issue(int i, const TileList& list, int tid) const {
+    const int k0 = __builtin_amdgcn_readfirstlane(list.tile[i]) * KT;
+    const bool guard = k0 + KT > S || __builtin_amdgcn_readfirstlane(list.lo[i]) < 0;      // lo: least entry of the tile's documents
     auto keep = [&](int r) { return k0 + r < S && (docs == nullptr || docs[k0 + r] >= 0); };
     kl.issue(k + k0 * ksr, keys(i), tid, guard, keep);
     vl.issue(v + k0 * vsr, values(i), tid, guard, keep);
-    if (docs && tid < KT) {      // (entries past the last key are never looked at: positions limit first)
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(docs + k0), 0, 4 * (S - k0), 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(keys(i) + 2 * TILE + (tid >> 6) * 256), 4, 4 * tid, 0, 0, 0);
+    if (docs && tid < KT)        // (entries past the last key are never looked at: positions limit first)
+      Source(docs + k0, 4 * (S - k0)).load4(4 * tid, __builtin_amdgcn_readfirstlane((int)(keys(i) + 2 * TILE + (tid >> 6) * 256)));
+  }
+  // Before the first tile of a list, and before each: its stage has landed, the loads of the one that takes the stage before it begin.
+  __device__ __forceinline__ void start(const TileList& list, int count, int tid) const {
+    for (int i = 0; i < STAGES - 1 && i < count; ++i) issue(i, list, tid);
+  }
+  __device__ __forceinline__ void next(int i, const TileList& list, int count, int tid) const {
+    if constexpr (STAGES > 1) {
+      landed<PER, STAGES>(count - 1 - i);
+      if (i + STAGES - 1 < count) issue(i + STAGES - 1, list, tid);
+    } else {
+      __syncthreads();
+      issue(i, list, tid);
+      landed<PER, 1>(0);
     }
   }
 };
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
-// FEW = false: 128 rows, 32 per wavefront, tiles of 64 keys.  FEW = true: at most 32 rows (one query and its group, or a few);
-// the four wavefronts share them, each takes 32 keys of a tile of 128, and they join their results in LDS at the end.
+// FEW = false: 32 rows to each of NW wavefronts.  FEW = true: at most 32 rows (one query and its group, or a few); the four
+// wavefronts share them, each takes 32 keys of a tile of 128, and they join their results in LDS at the end.
 // Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
-template <typename T, int D, bool FEW>
+#ifndef FWD_KT
+#define FWD_KT 64
+#define FWD_ST 2
+#define FWD_OCC (sizeof(T) == 2 ? 2 : 1)
+#endif
+template <typename T, int D, bool FEW, int NW>
 struct Fwd {
-  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 128, BUFS = KT * Tile<T, D>::ROWB > 32768 ? 1 : 2;
-  using Keys = KeyTiles<T, D, KT, BUFS>;
+  static constexpr int KT = FEW ? 128 : FWD_KT, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB;
+  static constexpr int STAGES = FEW ? (TILE > 32768 ? 1 : 2) : FWD_ST;
+  using Keys = KeyTiles<T, D, KT, STAGES, NW>;
   static constexpr int JOIN = FEW ? 4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 : 0;
   static constexpr int LDS = Keys::LDS > JOIN ? Keys::LDS : JOIN;
 };
 
-template <typename T, int D, bool CAP, bool FEW>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_forms_fwd(FormArgs a) {
-  using F = Fwd<T, D, FEW>;
+// largest of a lane's 16 scores and of those of the lane that holds the row's other 16
+__device__ __forceinline__ float row_top(const f32x16_t& s) {
+  float x = fmaxf(fmaxf(s[0], s[1]), s[2]), y = fmaxf(fmaxf(s[3], s[4]), s[5]);
+  x = fmaxf(fmaxf(x, s[6]), s[7]);
+  y = fmaxf(fmaxf(y, s[8]), s[9]);
+  x = fmaxf(fmaxf(x, s[10]), s[11]);
+  y = fmaxf(fmaxf(y, s[12]), s[13]);
+  x = fmaxf(fmaxf(x, s[14]), s[15]);
+  x = fmaxf(x, y);
+  const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+
+template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
+__global__ void __launch_bounds__(64 * NW, FEW ? 2 : FWD_OCC) k_forms_fwd(FormArgs a) {
+  using F = Fwd<T, D, FEW, NW>;
+  static_assert(!FEW || NW == 4, "the wavefronts that share 32 rows");
   constexpr int NK = FEW ? 1 : F::KT / 32;       // blocks of 32 keys of a tile that a wavefront takes
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
-  __shared__ int span_s[4][4];
+  __shared__ int span_s[NW][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + F::ROWS - 1) / F::ROWS;
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int split = id % a.splits;
-  id /= a.splits;
-  const int rt = a.causal ? n_rt - 1 - id % n_rt : id % n_rt;     // the longest rows first
-  id /= n_rt;
-  const int hk = id % a.nkv, b = id / a.nkv;
+  int bh, at;
+  tile_order(blockIdx.x, a.B * a.nkv, n_rt * a.splits, a.causal, bh, at);
+  const int split = at % a.splits, rt = a.causal ? n_rt - 1 - at / a.splits : at / a.splits;     // the longest rows first
+  const int hk = bh % a.nkv, b = bh / a.nkv;
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const RowOf r = row_of(a, rt * F::ROWS + (FEW ? 0 : wave * 32) + (lane & 31), b, hk, prefix);
-  const Span ws = wave_span(r), gs = group_span(ws, span_s, wave, lane);
+  const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
   Frags<T, D> qf;
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
   const Score sc = make_score(a.scale, a.cap);
-  const float factor = score_factor<CAP>(a, sc);
+  const float factor = score_factor<CAP, SLOPES>(sc);
+  const Lane<T, D> ln(lane);
   typename F::Keys kv;
   kv.init(a, b, hk, lds, tid);
 
@@ -460,63 +605,57 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) k_forms_fwd(FormA
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = zero16();
   float m_run = NO_MAX, l_run = 0.f;
+  // The exponentials' reference moves only when a score passes it by 2^8: any reference within that gives the same sums.
+  auto refer = [&](float top) {
+    if (__any(top > m_run + 8.f)) {
+      const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[db][j] *= alpha;
+    }
+  };
+  auto powers = [&](f32x16_t& s) {
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -m_run));
+      sum[j & 3] += s[j];
+    }
+    l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
   const int n_tiles = (a.S + F::KT - 1) / F::KT, per = (n_tiles + a.splits - 1) / a.splits;
   const int t_end = min(n_tiles, (split + 1) * per);
   for (int base = split * per; base < t_end; base += LIST) {
     const int t = base + tid;
     int lo = 0, hi = 0, take = 0;
-    if (t < t_end) {
+    if (tid < LIST && t < t_end) {
       positions_range(a, b, t * F::KT, min(a.S, (t + 1) * F::KT) - 1, lo, hi);
       take = tile_state(a, gs, t * F::KT, F::KT, lo, hi) != 0;
     }
     const int count = make_list(list, take, t, lo, hi, tid);
-    if (F::BUFS > 1 && count > 0) kv.issue(0, list.tile[0] * F::KT, list.lo[0], tid);
+    // first key of tile i, and whether it has to be masked for this wavefront (a tile hidden from all its rows: like a masked one)
+    auto first_key = [&](int i) { return __builtin_amdgcn_readfirstlane(list.tile[i]) * F::KT; };
+    auto state_of = [&](int i) {
+      return tile_state(a, ws, first_key(i), F::KT, __builtin_amdgcn_readfirstlane(list.lo[i]), __builtin_amdgcn_readfirstlane(list.hi[i]));
+    };
+    const int kb0 = FEW ? wave : 0;
+    kv.start(list, count, tid);
     for (int i = 0; i < count; ++i) {
-      const int k0 = list.tile[i] * F::KT;
-      if constexpr (F::BUFS > 1) {
-        landed();
-        if (i + 1 < count) kv.issue(i + 1, list.tile[i + 1] * F::KT, list.lo[i + 1], tid);
-      } else {
-        __syncthreads();
-        kv.issue(i, k0, list.lo[i], tid);
-        landed();
-      }
-      const int state = tile_state(a, ws, k0, F::KT, list.lo[i], list.hi[i]);
+      kv.next(i, list, count, tid);
+      const int k0 = first_key(i), state = state_of(i);
       if (state == 0) continue;
-      const int kb0 = FEW ? wave : 0;
-      f32x16_t s[NK];
 #pragma unroll
-      for (int kb = 0; kb < NK; ++kb) s[kb] = dot_rows<T, D>(kv.keys(i), 32 * (kb0 + kb), qf, lane);
-#pragma unroll
-      for (int kb = 0; kb < NK; ++kb)
-        scores<CAP, false>(a, sc, r, kv.ids(i) + 32 * (kb0 + kb), k0 + 32 * (kb0 + kb), half, state == 1, s[kb], unused);
-      float top = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < NK; ++kb)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) top = fmaxf(top, s[kb][j]);
-      top = factor * fmaxf(top, __shfl_xor(top, 32, 64));
-      // The exponentials' reference moves only when a score passes it by 2^8: any reference within that gives the same sums.
-      if (__any(top > m_run + 8.f)) {
-        const float m_new = fmaxf(m_run, top), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= alpha;
-        m_run = m_new;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) o[db][j] *= alpha;
+      for (int kb = 0; kb < NK; ++kb) {
+        const int row0 = 32 * (kb0 + kb);
+        f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln);
+        scores<CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, half, state == 1, s, unused);
+        refer(factor * row_top(s));
+        powers(s);
+        add_outer<T, D>(o, kv.values(i), row0, s, ln);
       }
-      float sum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < NK; ++kb)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          s[kb][j] = __builtin_amdgcn_exp2f(fmaf(s[kb][j], factor, -m_run));
-          sum += s[kb][j];
-        }
-      l_run += sum;
-#pragma unroll
-      for (int kb = 0; kb < NK; ++kb) add_outer<T, D>(o, kv.values(i), 32 * (kb0 + kb), s[kb], lane);
     }
   }
   l_run += __shfl_xor(l_run, 32, 64);
@@ -618,31 +757,36 @@ __device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
 // bf16: the stored output is rounded, so sum_d dO O is not quite the delta that makes a row of p (dp - delta) add up to zero, and
 // in rows that look at few keys what is left is of the gradient's own size.  The kernel finds it, rest = sum p (dp - delta),
 // and takes it out: delta grows by rest, dQ loses rest * sum p damp k, for which those sums are formed beside dQ.
-template <typename T, int D>
-struct Bwd {
-  static constexpr int KT = 64;
-  using Keys = KeyTiles<T, D, KT, 2>;
+// bf16 at width 128: the registers of dQ, of those sums and of the queries leave no room for dO's, which stay in LDS (SPARE).
+template <typename T, int D, int NW>
+struct BwdQ {
+  static constexpr int KT = 64, STAGES = 2;
+  static constexpr bool MEND = sizeof(T) == 2, SPARE = sizeof(T) == 2 && D == 128;
+  using Keys = KeyTiles<T, D, KT, STAGES, NW>;
+  static constexpr int LDS = Keys::LDS + (SPARE ? NW * 32 * Tile<T, D>::ROWB : 0);
 };
-template <typename T, int D, bool CAP>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_forms_bwd_q(FormArgs a) {
-  constexpr int KT = Bwd<T, D>::KT;
-  constexpr bool MEND = sizeof(T) == 2;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+template <typename T, int D, bool CAP, bool SLOPES, int NW>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_q(FormArgs a) {
+  using Q = BwdQ<T, D, NW>;
+  constexpr int KT = Q::KT;
+  constexpr bool MEND = Q::MEND;
+  extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
-  __shared__ int span_s[4][4];
+  __shared__ int span_s[NW][4];
+  unsigned char* const Gs = lds + Q::Keys::LDS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + 127) / 128;
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int rt = a.causal ? n_rt - 1 - id % n_rt : id % n_rt;
-  id /= n_rt;
-  const int hk = id % a.nkv, b = id / a.nkv;
+  const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + 32 * NW - 1) / (32 * NW);
+  int bh, at;
+  tile_order(blockIdx.x, a.B * a.nkv, n_rt, a.causal, bh, at);
+  const int rt = a.causal ? n_rt - 1 - at : at, hk = bh % a.nkv, b = bh / a.nkv;
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
-  const RowOf r = row_of(a, rt * 128 + wave * 32 + (lane & 31), b, hk, prefix);
-  const Span ws = wave_span(r), gs = group_span(ws, span_s, wave, lane);
+  const RowOf r = row_of(a, rt * 32 * NW + wave * 32 + (lane & 31), b, hk, prefix);
+  const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
   const Score sc = make_score(a.scale, a.cap);
-  const float factor = score_factor<CAP>(a, sc);
-  typename Bwd<T, D>::Keys kv;
+  const float factor = score_factor<CAP, SLOPES>(sc);
+  const Lane<T, D> ln(lane);
+  typename Q::Keys kv;
   kv.init(a, b, hk, lds, tid);
 
   Frags<T, D> qf, gf;
@@ -652,7 +796,6 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
     l2 = a.lse[lrow] * LOG2E;
     if (l2 == -INFINITY) l2 = INFINITY;       // sees no key: probabilities zero
   }
-  load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
   load_frags<T, D>(gf, head_ptr<T>(a.g, b, r.head) + (long long)r.qi * a.g.sr, half, a.w, r.live);
   {
     Frags<T, D> of;
@@ -661,6 +804,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
     for (int s = 0; s < Tile<T, D>::NS; ++s) delta += dot_chunk<T>(gf[s], of[s]);
     delta += __shfl_xor(delta, 32, 64);
   }
+  if constexpr (Q::SPARE) {      // (a wavefront reads back its own rows only)
+#pragma unroll
+    for (int s = 0; s < Tile<T, D>::NS; ++s) *Tile<T, D>::at(Gs, wave * 32 + (lane & 31), 2 * s + half) = gf[s];
+  }
+  load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
 
   f32x16_t dq[D / 32], pk[MEND ? D / 32 : 1], damp;
 #pragma unroll
@@ -671,23 +819,23 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
   for (int base = 0; base < n_tiles; base += LIST) {
     const int t = base + tid;
     int lo = 0, hi = 0, take = 0;
-    if (t < n_tiles) {
+    if (tid < LIST && t < n_tiles) {
       positions_range(a, b, t * KT, min(a.S, (t + 1) * KT) - 1, lo, hi);
       take = tile_state(a, gs, t * KT, KT, lo, hi) != 0;
     }
     const int count = make_list(list, take, t, lo, hi, tid);
-    if (count > 0) kv.issue(0, list.tile[0] * KT, list.lo[0], tid);
+    kv.start(list, count, tid);
     for (int i = 0; i < count; ++i) {
       const int k0 = list.tile[i] * KT;
-      landed();
-      if (i + 1 < count) kv.issue(i + 1, list.tile[i + 1] * KT, list.lo[i + 1], tid);
+      kv.next(i, list, count, tid);
       const int state = tile_state(a, ws, k0, KT, list.lo[i], list.hi[i]);
       if (state == 0) continue;
-#pragma unroll
+#pragma unroll Q::SPARE ? 1 : KT / 32
       for (int kb = 0; kb < KT / 32; ++kb) {
-        f32x16_t s = dot_rows<T, D>(kv.keys(i), 32 * kb, qf, lane);
-        f32x16_t dp = dot_rows<T, D>(kv.values(i), 32 * kb, gf, lane);
-        scores<CAP, true>(a, sc, r, kv.ids(i) + 32 * kb, k0 + 32 * kb, half, state == 1, s, damp);
+        f32x16_t s = dot_rows<T, D>(kv.keys(i), 32 * kb, qf, ln), dp;
+        if constexpr (Q::SPARE) dp = dot_tiles<T, D>(kv.values(i), 32 * kb, lds_addr(Gs) + wave * 32 * Tile<T, D>::ROWB, ln);
+        else dp = dot_rows<T, D>(kv.values(i), 32 * kb, gf, ln);
+        scores<CAP, SLOPES, true>(a, sc, r, kv.ids(i) + 32 * kb, k0 + 32 * kb, half, state == 1, s, damp);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
@@ -699,8 +847,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
           s[j] = p;
           dp[j] = ds;
         }
-        add_outer<T, D>(dq, kv.keys(i), 32 * kb, dp, lane);
-        if constexpr (MEND) add_outer<T, D>(pk, kv.keys(i), 32 * kb, s, lane);
+        if constexpr (MEND) add_outer2<T, D>(dq, pk, kv.keys(i), 32 * kb, dp, s, ln);
+        else add_outer<T, D>(dq, kv.keys(i), 32 * kb, dp, ln);
       }
     }
   }
@@ -718,26 +866,37 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
 }
 
 // ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
-// 128 keys, 32 per wavefront, over tiles of the 64 / G queries whose rows fit 64 (G: heads of the group).
+// 128 keys, over tiles of the 64 / G queries whose rows fit 64 (G: heads of the group).  NW = 4: 32 keys to a wavefront.  NW = 8
+// (bf16 at width 128): two wavefronts share 32 keys, one takes the first 32 rows of a tile and one the others, and they add
+// up at the end; the values stay in LDS, as the accumulators and the keys fill the registers.
+// Few workgroups: the rows are split over a.row_splits workgroups, whose sums k_forms_kv_join adds.
 struct RowMeta {
   float l2[64], delta[64], slope[64];
   int lim[64], id[64], pos[64];
 };
-template <typename T, int D, bool CAP>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
-  constexpr int RT = 64, TILE = RT * Tile<T, D>::ROWB;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+template <typename T, int D, int NW>
+struct BwdKv {
+  static constexpr int RT = 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
+  static constexpr bool SPARE = NW == 8;
+  static constexpr int LDS = 2 * STAGE + (SPARE ? 128 * Tile<T, D>::ROWB : 0);
+};
+template <typename T, int D, bool CAP, bool SLOPES, int NW>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
+  using K = BwdKv<T, D, NW>;
+  constexpr int RT = K::RT, TILE = K::TILE, NR = NW == 8 ? 1 : 2;      // blocks of 32 rows of a tile that a wavefront takes
+  extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ __attribute__((aligned(16))) RowMeta meta[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  unsigned char* const Vs = lds + 2 * K::STAGE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, blk = wave & 3, part = wave >> 2;
   const int G = a.nh / a.nkv, QT = RT / G, used = QT * G, n_kt = (a.S + 127) / 128, first = a.S - a.n;
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int kt = id % n_kt;
-  id /= n_kt;
-  const int hk = id % a.nkv, b = id / a.nkv;
+  int bh, at;
+  tile_order(blockIdx.x, a.B * a.nkv, n_kt * a.row_splits, a.causal, bh, at);     // (the first keys have the most rows)
+  const int kt = at / a.row_splits, split = at % a.row_splits;
+  const int hk = bh % a.nkv, b = bh / a.nkv;
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
-  const int kw = kt * 128 + wave * 32, key = kw + (lane & 31);      // this wavefront's keys, this lane's
+  const int kw = kt * 128 + blk * 32, key = kw + (lane & 31);      // this wavefront's keys, this lane's
   const bool in = key < a.S;
   const int kid = docs ? (in ? docs[key] : -1) : 0;
   const bool live = in && kid >= 0;
@@ -749,16 +908,22 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
   Frags<T, D> kf, vf;
   load_frags<T, D>(kf, head_ptr<T>(a.k, b, hk) + (long long)(in ? key : 0) * a.k.sr, half, a.w, live);
   load_frags<T, D>(vf, head_ptr<T>(a.v, b, hk) + (long long)(in ? key : 0) * a.v.sr, half, a.w, live);
+  if constexpr (K::SPARE) {
+    if (part == 0)
+#pragma unroll
+      for (int s = 0; s < Tile<T, D>::NS; ++s) *Tile<T, D>::at(Vs, blk * 32 + (lane & 31), 2 * s + half) = vf[s];
+  }
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
 
-  Loader<T, D, RT> ql, gl;
+  const Lane<T, D> ln(lane);
+  Loader<T, D, RT, NW> ql, gl;
   ql.init(tid, a.q.sr * (int)sizeof(T), G, a.q.sh * (int)sizeof(T), used, a.w);
   gl.init(tid, a.g.sr * (int)sizeof(T), G, a.g.sh * (int)sizeof(T), used, a.w);
   const T* qbase = head_ptr<T>(a.q, b, hk * G);
   const T* gbase = head_ptr<T>(a.g, b, hk * G);
-  auto tiles = [&](int i) { return lds + (i & 1) * 2 * TILE; };
+  auto tiles = [&](int i) { return lds + (i & 1) * K::STAGE; };
   // queries q0 .. q0 + QT - 1 of all heads of the group; what the mask needs of a row waits in the registers of wavefront 0
   RowOf mr;
   float ml2 = 0.f, mdelta = 0.f;
@@ -772,8 +937,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
     }
     const bool guard = q0 + QT > a.n || lo < 0;
     auto keep = [&](int r) { return q0 + r / G < a.n && (docs == nullptr || docs[first + q0 + r / G] >= 0); };
-    ql.issue(qbase + q0 * a.q.sr, tiles(i), tid, guard, keep);
-    gl.issue(gbase + q0 * a.g.sr, tiles(i) + TILE, tid, guard, keep);
+    ql.issue(qbase + q0 * a.q.sr, lds_addr(tiles(i)), tid, guard, keep);
+    gl.issue(gbase + q0 * a.g.sr, lds_addr(tiles(i)) + TILE, tid, guard, keep);
   };
   auto commit = [&](int i) {
     if (tid >= RT) return;
@@ -786,11 +951,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
     m.pos[tid] = mr.pos;
   };
 
-  const int n_tiles = (a.n + QT - 1) / QT;
+  const int all_tiles = (a.n + QT - 1) / QT, n_tiles = (all_tiles - split + a.row_splits - 1) / a.row_splits;   // every row_splits-th
   for (int base = 0; base < n_tiles; base += LIST) {
-    const int t = base + tid;
+    const int t = (base + tid) * a.row_splits + split;
     int lo = 0, hi = 0, take = 0;
-    if (t < n_tiles) {
+    if (tid < LIST && base + tid < n_tiles) {
       const int p0 = first + t * QT, p1 = first + min(a.n, t * QT + QT) - 1;
       positions_range(a, b, p0, p1, lo, hi);
       take = kt * 128 < key_limit(a, p1, prefix) && (!docs || (hi >= 0 && khi >= 0 && lo <= khi && hi >= klo));
@@ -803,32 +968,35 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
     for (int i = 0; i < count; ++i) {
       const int q0 = list.tile[i] * QT, p0 = first + q0, p1 = first + min(a.n, q0 + QT) - 1;
       const int lo_t = list.lo[i], hi_t = list.hi[i];
-      landed();
+      __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): what commit() wrote
+      landed<0, 2>(0);
       if (i + 1 < count) issue(i + 1, list.tile[i + 1] * QT, list.lo[i + 1]);
       const RowMeta& m = meta[i & 1];
+      const uint32_t tile = lds_addr(tiles(i));
       const bool hidden = kw >= key_limit(a, p1, prefix) || kid_hi < 0 || (docs && (hi_t < kid_lo || lo_t > kid_hi));
       const bool mask = kw + 32 > key_limit(a, p0, prefix) || (docs && !(lo_t == hi_t && lo_t == kid_lo && lo_t == kid_hi));
       if (!hidden) {
 #pragma unroll 1
-        for (int rb = 0; rb < RT / 32; ++rb) {
-          f32x16_t s = dot_rows<T, D>(tiles(i), 32 * rb, kf, lane);
-          f32x16_t dp = dot_rows<T, D>(tiles(i) + TILE, 32 * rb, vf, lane);
+        for (int rb = NR == 1 ? part : 0; rb < (NR == 1 ? part + 1 : 2); ++rb) {
+          f32x16_t s = dot_rows<T, D>(tile, 32 * rb, kf, ln), dp;
+          if constexpr (K::SPARE) dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln);
+          else dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const int at = 32 * rb + 8 * g + 4 * half;
-            const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at);
+            const int at4 = 32 * rb + 8 * g + 4 * half;
+            const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at4), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at4);
             float x[4], d[4] = {1.f, 1.f, 1.f, 1.f};
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = score2<CAP>(sc, s[4 * g + j], d[j]);
-            if (a.slopes) {
-              const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at);
-              const int4 ps = *reinterpret_cast<const int4*>(m.pos + at);
+            if constexpr (SLOPES) {
+              const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
+              const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
               const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
 #pragma unroll
               for (int j = 0; j < 4; ++j) x[j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), x[j]);
             }
             if (mask) {
-              const int4 lm = *reinterpret_cast<const int4*>(m.lim + at), qi = *reinterpret_cast<const int4*>(m.id + at);
+              const int4 lm = *reinterpret_cast<const int4*>(m.lim + at4), qi = *reinterpret_cast<const int4*>(m.id + at4);
               const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
 #pragma unroll
               for (int j = 0; j < 4; ++j) x[j] = key < lim[j] && (!docs || qid[j] == kid) ? x[j] : -INFINITY;
@@ -840,21 +1008,69 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && D == 64 ? 2 : 1) k_form
               dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * d[j];
             }
           }
-          add_outer<T, D>(dv, tiles(i) + TILE, 32 * rb, s, lane);
-          add_outer<T, D>(dk, tiles(i), 32 * rb, dp, lane);
+          add_outer<T, D>(dv, tile + TILE, 32 * rb, s, ln);
+          add_outer<T, D>(dk, tile, 32 * rb, dp, ln);
         }
       }
       if (i + 1 < count) commit(i + 1);
     }
   }
+  if constexpr (NW == 8) {
+    // the second part's sums onto the first's: 32 keys x 128 d a wavefront, dK and then dV through the same 64 KB
+    constexpr int LD = 16 * D / 32 * 64;
+    float* const mine = reinterpret_cast<float*>(lds) + blk * LD + lane * 4;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      f32x16_t (&acc)[D / 32] = which ? dv : dk;
+      __syncthreads();
+      if (part == 1)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<f32x4_t*>(mine + (4 * i + g) * 256) = f32x4_t{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+      __syncthreads();
+      if (part == 0)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(mine + (4 * i + g) * 256);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][4 * g + j] += x[j];
+          }
+    }
+    if (part == 1) return;
+  }
   if (!in) return;
-  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, a.scale, live);
-  store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)key * a.dv.sr, dv, half, a.w, 1.f, live);
+  if (a.row_splits > 1) {
+    const size_t all = (size_t)a.B * a.nkv * a.S, row = ((size_t)b * a.nkv + hk) * a.S + key;
+    float* const out = a.part + ((size_t)split * 2 * all + row) * a.w;
+    store_row<float, D>(out, dk, half, a.w, a.scale, live);
+    store_row<float, D>(out + all * a.w, dv, half, a.w, 1.f, live);
+  } else {
+    store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, a.scale, live);
+    store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)key * a.dv.sr, dv, half, a.w, 1.f, live);
+  }
+}
+
+// Sums of the workgroups that shared a key's rows, in their order; four elements a lane.
+template <typename T>
+__global__ void __launch_bounds__(256) k_forms_kv_join(FormArgs a) {
+  const size_t all = (size_t)a.B * a.nkv * a.S * a.w, e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (e >= 2 * all) return;
+  f32x4_t x = *reinterpret_cast<const f32x4_t*>(a.part + e);
+  for (int s = 1; s < a.row_splits; ++s) x += *reinterpret_cast<const f32x4_t*>(a.part + s * 2 * all + e);
+  const bool v = e >= all;
+  const size_t i = v ? e - all : e, row = i / a.w;
+  const int d = (int)(i % a.w), key = (int)(row % a.S), hk = (int)(row / a.S) % a.nkv, b = (int)(row / ((size_t)a.S * a.nkv));
+  const FormHeads& out = v ? a.dv : a.dk;
+  store4(head_out<T>(out, b, hk) + (long long)key * out.sr + d, x[0], x[1], x[2], x[3]);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
 template <auto Kernel>
-inline hipError_t launch(size_t blocks, int lds, const FormArgs& a, hipStream_t s) {
+inline hipError_t launch(int threads, size_t blocks, int lds, const FormArgs& a, hipStream_t s) {
   static std::atomic<bool> allowed[64];      // once per kernel and device: more than 64 KB of LDS has to be asked for
   if (lds > 0) {
     int dev = 0;
@@ -866,36 +1082,58 @@ inline hipError_t launch(size_t blocks, int lds, const FormArgs& a, hipStream_t 
       if (dev >= 0 && dev < 64) allowed[dev].store(true, std::memory_order_relaxed);
     }
   }
-  Kernel<<<dim3((unsigned)blocks), dim3(256), lds, s>>>(a);
+  Kernel<<<dim3((unsigned)blocks), dim3((unsigned)threads), lds, s>>>(a);
   return hipGetLastError();
 }
 
-template <typename T, int D, bool CAP>
-hipError_t fwd_w(const FormArgs& a, hipStream_t s) {
-  const int rows = a.n * (a.nh / a.nkv);
-  const size_t heads = (size_t)a.B * a.nkv * a.splits;
-  hipError_t e = rows <= 32 ? launch<k_forms_fwd<T, D, CAP, true>>(heads, Fwd<T, D, true>::LDS, a, s)
-                            : launch<k_forms_fwd<T, D, CAP, false>>(heads * ((rows + 127) / 128), Fwd<T, D, false>::LDS, a, s);
-  if (e != hipSuccess || a.splits == 1) return e;
-  return launch<k_forms_join<T>>(((size_t)a.B * a.nkv * rows + 3) / 4, 0, a, s);
+// Whether 256 rows a workgroup (eight wavefronts, half the reads of the keys) leave one for every compute unit.
+bool wide_rows(bool b16, int w, size_t heads, int rows);
+
+template <typename T, int D, bool CAP, bool SLOPES>
+struct Launch {
+  static constexpr bool WIDE = sizeof(T) == 2 && D == 128;
+  static constexpr int NW = WIDE ? 8 : 4;
+  static size_t tiles(int rows, int nw) { return ((size_t)rows + 32 * nw - 1) / (32 * nw); }
+  static hipError_t fwd(const FormArgs& a, hipStream_t s) {
+    const int rows = a.n * (a.nh / a.nkv);
+    const size_t heads = (size_t)a.B * a.nkv;
+    hipError_t e;
+    if (rows <= 32) e = launch<k_forms_fwd<T, D, CAP, SLOPES, true, 4>>(256, heads * a.splits, Fwd<T, D, true, 4>::LDS, a, s);
+    else if (WIDE && wide_rows(true, a.w, heads, rows))
+      e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, NW) * a.splits, Fwd<T, D, false, NW>::LDS, a, s);
+    else e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 4) * a.splits, Fwd<T, D, false, 4>::LDS, a, s);
+    if (e != hipSuccess || a.splits == 1) return e;
+    return launch<k_forms_join<T>>(256, (heads * rows + 3) / 4, 0, a, s);
+  }
+  static hipError_t bwd(const FormArgs& a, hipStream_t s) {
+    const int rows = a.n * (a.nh / a.nkv);
+    const size_t heads = (size_t)a.B * a.nkv;
+    hipError_t e;
+    if (WIDE && wide_rows(true, a.w, heads, rows))
+      e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, NW>>(64 * NW, heads * tiles(rows, NW), BwdQ<T, D, NW>::LDS, a, s);
+    else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, 4>>(256, heads * tiles(rows, 4), BwdQ<T, D, 4>::LDS, a, s);
+    if (e != hipSuccess) return e;
+    e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, NW>>(64 * NW, heads * ((a.S + 127) / 128) * a.row_splits, BwdKv<T, D, NW>::LDS, a, s);
+    if (e != hipSuccess || a.row_splits == 1) return e;
+    return launch<k_forms_kv_join<T>>(256, (heads * a.S * a.w / 2 + 255) / 256, 0, a, s);
+  }
+};
+template <typename T, int D, typename F>
+hipError_t pick_w(const FormArgs& a, F f) {
+  if (a.cap > 0.f) return a.slopes ? f(Launch<T, D, true, true>{}) : f(Launch<T, D, true, false>{});
+  return a.slopes ? f(Launch<T, D, false, true>{}) : f(Launch<T, D, false, false>{});
 }
-template <typename T, int D, bool CAP>
-hipError_t bwd_w(const FormArgs& a, hipStream_t s) {
-  const int rows = a.n * (a.nh / a.nkv);
-  const size_t heads = (size_t)a.B * a.nkv;
-  const hipError_t e = launch<k_forms_bwd_q<T, D, CAP>>(heads * ((rows + 127) / 128), Bwd<T, D>::Keys::LDS, a, s);
-  if (e != hipSuccess) return e;
-  return launch<k_forms_bwd_kv<T, D, CAP>>(heads * ((a.S + 127) / 128), 4 * 64 * Tile<T, D>::ROWB, a, s);
+template <typename T, typename F>
+hipError_t pick(const FormArgs& a, F f) {
+  return a.w <= 64 ? pick_w<T, 64>(a, f) : pick_w<T, 128>(a, f);
 }
 template <typename T>
 hipError_t fwd_t(const FormArgs& a, hipStream_t s) {
-  if (a.w <= 64) return a.cap > 0.f ? fwd_w<T, 64, true>(a, s) : fwd_w<T, 64, false>(a, s);
-  return a.cap > 0.f ? fwd_w<T, 128, true>(a, s) : fwd_w<T, 128, false>(a, s);
+  return pick<T>(a, [&](auto l) { return decltype(l)::fwd(a, s); });
 }
 template <typename T>
 hipError_t bwd_t(const FormArgs& a, hipStream_t s) {
-  if (a.w <= 64) return a.cap > 0.f ? bwd_w<T, 64, true>(a, s) : bwd_w<T, 64, false>(a, s);
-  return a.cap > 0.f ? bwd_w<T, 128, true>(a, s) : bwd_w<T, 128, false>(a, s);
+  return pick<T>(a, [&](auto l) { return decltype(l)::bwd(a, s); });
 }
 
 }  // namespace forms

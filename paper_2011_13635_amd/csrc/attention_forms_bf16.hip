@@ -33,6 +33,18 @@ int form_splits(int dtype, int B, int n, int S, int nh, int nkv, int w) {
   return blocks >= 256 || splits < 1 ? 1 : (int)splits;
 }
 
+// The key side's workgroups take 128 keys each; below two for each of 256 compute units (causal: the first keys' are the longest)
+// the rows are split, as far as every part keeps eight tiles of 64.
+int form_row_splits(int B, int n, int S, int nh, int nkv) {
+  const long long blocks = (long long)B * nkv * ((S + 127) / 128), tiles = (long long)n * (nh / nkv) / 64;
+  const long long want = (512 + blocks - 1) / blocks, most = tiles / 8;
+  const long long splits = want < most ? want : most;
+  return splits < 1 ? 1 : (int)splits;
+}
+namespace forms {
+bool wide_rows(bool b16, int w, size_t heads, int rows) { return b16 && w > 64 && heads * ((size_t)rows / 256) >= 256; }
+}  // namespace forms
+
 hipError_t form_fwd_bf16(const FormArgs& a, hipStream_t s) { return forms::fwd_t<bf16>(a, s); }
 hipError_t form_bwd_bf16(const FormArgs& a, hipStream_t s) { return forms::bwd_t<bf16>(a, s); }
 

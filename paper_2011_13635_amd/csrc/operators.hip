@@ -192,7 +192,7 @@ namespace {
 struct Workspace {
   size_t ranges, part, part_ml, delta, total;
 };
-Workspace attention_layout(int precision, int batch, int queries, int keys, int heads, int kv_heads, int width, bool backward, int* splits) {
+Workspace attention_layout(int precision, int batch, int queries, int keys, int heads, int kv_heads, int width, bool backward, int* splits, int* row_splits) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   Workspace w{};
   const size_t rows = (size_t)batch * heads * queries;
@@ -203,6 +203,11 @@ Workspace attention_layout(int precision, int batch, int queries, int keys, int 
     at += up(rows * *splits * width * sizeof(float));
     w.part_ml = at;
     at += up(rows * *splits * sizeof(float2));
+  }
+  *row_splits = backward ? form_row_splits(batch, queries, keys, heads, kv_heads) : 1;
+  if (*row_splits > 1) {
+    w.part = at;
+    at += up((size_t)2 * *row_splits * batch * kv_heads * keys * width * sizeof(float));
   }
   if (backward) {
     w.delta = at;
@@ -216,9 +221,9 @@ Workspace attention_layout(int precision, int batch, int queries, int keys, int 
 extern "C" int mslt_attention_workspace(int precision, int batch, int queries, int keys, int heads, int kv_heads, int width, int backward,
                                         size_t* bytes) {
   if (!bytes) return fail(MSLT_ERR_ARG, "attention_workspace: bytes is null");
-  int rc = attention_sizes("attention_workspace", precision, batch, queries, keys, heads, kv_heads, width), splits = 1;
+  int rc = attention_sizes("attention_workspace", precision, batch, queries, keys, heads, kv_heads, width), splits = 1, row_splits = 1;
   if (rc) return rc;
-  *bytes = attention_layout(precision, batch, queries, keys, heads, kv_heads, width, backward != 0, &splits).total;
+  *bytes = attention_layout(precision, batch, queries, keys, heads, kv_heads, width, backward != 0, &splits, &row_splits).total;
   return MSLT_OK;
 }
 
@@ -237,7 +242,7 @@ static int attention_args(const char* who, int precision, int batch, int queries
   if (!(f->scale > 0.f) || !std::isfinite(f->scale)) return fail(MSLT_ERR_ARG, "%s: scale must be above 0", who);
   if (!(f->cap >= 0.f) || !std::isfinite(f->cap)) return fail(MSLT_ERR_ARG, "%s: cap must be 0 or above", who);
   if (f->prefix && !f->causal) return fail(MSLT_ERR_ARG, "%s: a prefix needs causal", who);
-  const Workspace w = attention_layout(precision, batch, queries, keys, heads, kv_heads, width, backward, &a.splits);
+  const Workspace w = attention_layout(precision, batch, queries, keys, heads, kv_heads, width, backward, &a.splits, &a.row_splits);
   if (!workspace || workspace_bytes < w.total || reinterpret_cast<uintptr_t>(workspace) % 16)
     return fail(MSLT_ERR_ARG, "%s: needs a workspace of %zu bytes, 16-byte aligned", who, w.total);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
