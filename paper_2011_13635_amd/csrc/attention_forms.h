@@ -545,18 +545,14 @@ struct KeyTiles {
 };
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
-// FEW = false: 32 rows to each of NW wavefronts.  FEW = true: at most 32 rows (one query and its group, or a few); the four
-// wavefronts share them, each takes 32 keys of a tile of 128, and they join their results in LDS at the end.
+// FEW = false: 32 rows to each of NW wavefronts.  FEW = true (few rows in all): four wavefronts share 32 rows, each takes 32 keys of
+// a tile of 128, and they join their results in LDS at the end.
 // Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
-#ifndef FWD_KT
-#define FWD_KT 64
-#define FWD_ST 2
-#define FWD_OCC (sizeof(T) == 2 ? 2 : 1)
-#endif
 template <typename T, int D, bool FEW, int NW>
 struct Fwd {
-  static constexpr int KT = FEW ? 128 : FWD_KT, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB;
-  static constexpr int STAGES = FEW ? (TILE > 32768 ? 1 : 2) : FWD_ST;
+  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB, STAGES = TILE > 32768 ? 1 : 2;
+  // wavefronts that share a SIMD: as many as the registers of the accumulators allow
+  static constexpr int WAVES = sizeof(T) == 4 ? 1 : D == 64 && !FEW ? 4 : 2;
   using Keys = KeyTiles<T, D, KT, STAGES, NW>;
   static constexpr int JOIN = FEW ? 4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 : 0;
   static constexpr int LDS = Keys::LDS > JOIN ? Keys::LDS : JOIN;
@@ -576,7 +572,7 @@ __device__ __forceinline__ float row_top(const f32x16_t& s) {
 }
 
 template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
-__global__ void __launch_bounds__(64 * NW, FEW ? 2 : FWD_OCC) k_forms_fwd(FormArgs a) {
+__global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_fwd(FormArgs a) {
   using F = Fwd<T, D, FEW, NW>;
   static_assert(!FEW || NW == 4, "the wavefronts that share 32 rows");
   constexpr int NK = FEW ? 1 : F::KT / 32;       // blocks of 32 keys of a tile that a wavefront takes
@@ -738,6 +734,34 @@ __global__ void __launch_bounds__(256) k_forms_join(FormArgs a) {
   if (lane == 0) a.lse[((size_t)b * a.nh + head) * a.n + qi] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
 }
 
+// Sums of PARTS wavefronts that worked on the same rows (or keys), of which a workgroup has BLOCKS: the others' through LDS onto
+// part 0's, in their order.  Called by the whole workgroup.
+template <int D, int PARTS, int BLOCKS>
+__device__ __forceinline__ void add_parts(f32x16_t (&acc)[D / 32], unsigned char* lds, int part, int blk, int lane) {
+  constexpr int FLOATS = 32 * D;
+  float* const mine = reinterpret_cast<float*>(lds) + blk * FLOATS + lane * 4;
+  __syncthreads();
+  if (part > 0)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4_t*>(mine + (part - 1) * BLOCKS * FLOATS + (4 * i + g) * 256) =
+            f32x4_t{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+  __syncthreads();
+  if (part == 0)
+#pragma unroll
+    for (int p = 0; p < PARTS - 1; ++p)
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4_t x = *reinterpret_cast<const f32x4_t*>(mine + p * BLOCKS * FLOATS + (4 * i + g) * 256);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][4 * g + j] += x[j];
+        }
+}
+
 // ---- backward, query side: delta = sum_d dO O, dQ -----------------------------------------------------------------------
 template <typename T>
 __device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
@@ -758,30 +782,33 @@ __device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
 // in rows that look at few keys what is left is of the gradient's own size.  The kernel finds it, rest = sum p (dp - delta),
 // and takes it out: delta grows by rest, dQ loses rest * sum p damp k, for which those sums are formed beside dQ.
 // bf16 at width 128: the registers of dQ, of those sums and of the queries leave no room for dO's, which stay in LDS (SPARE).
-template <typename T, int D, int NW>
+// FEW as in the forward.
+template <typename T, int D, bool FEW, int NW>
 struct BwdQ {
-  static constexpr int KT = 64, STAGES = 2;
+  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB, STAGES = TILE > 32768 ? 1 : 2;
   static constexpr bool MEND = sizeof(T) == 2, SPARE = sizeof(T) == 2 && D == 128;
   using Keys = KeyTiles<T, D, KT, STAGES, NW>;
-  static constexpr int LDS = Keys::LDS + (SPARE ? NW * 32 * Tile<T, D>::ROWB : 0);
+  static constexpr int LDS = Keys::LDS + (SPARE ? ROWS * Tile<T, D>::ROWB : 0);
+  static_assert(!FEW || Keys::LDS >= 3 * 32 * D * 4 + 3 * 256, "the join's room");
 };
-template <typename T, int D, bool CAP, bool SLOPES, int NW>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_q(FormArgs a) {
-  using Q = BwdQ<T, D, NW>;
-  constexpr int KT = Q::KT;
+template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8) ? 2 : 1) k_forms_bwd_q(FormArgs a) {
+  using Q = BwdQ<T, D, FEW, NW>;
+  static_assert(!FEW || NW == 4, "the wavefronts that share 32 rows");
+  constexpr int KT = Q::KT, NK = FEW ? 1 : KT / 32;
   constexpr bool MEND = Q::MEND;
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int span_s[NW][4];
   unsigned char* const Gs = lds + Q::Keys::LDS;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
-  const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + 32 * NW - 1) / (32 * NW);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, part = FEW ? wave : 0, row_blk = FEW ? 0 : wave;
+  const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + Q::ROWS - 1) / Q::ROWS;
   int bh, at;
   tile_order(blockIdx.x, a.B * a.nkv, n_rt, a.causal, bh, at);
   const int rt = a.causal ? n_rt - 1 - at : at, hk = bh % a.nkv, b = bh / a.nkv;
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
-  const RowOf r = row_of(a, rt * 32 * NW + wave * 32 + (lane & 31), b, hk, prefix);
+  const RowOf r = row_of(a, rt * Q::ROWS + row_blk * 32 + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
   const Score sc = make_score(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
@@ -804,9 +831,9 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_q
     for (int s = 0; s < Tile<T, D>::NS; ++s) delta += dot_chunk<T>(gf[s], of[s]);
     delta += __shfl_xor(delta, 32, 64);
   }
-  if constexpr (Q::SPARE) {      // (a wavefront reads back its own rows only)
+  if constexpr (Q::SPARE) {      // (a wavefront reads back what it wrote, or the same that the others write)
 #pragma unroll
-    for (int s = 0; s < Tile<T, D>::NS; ++s) *Tile<T, D>::at(Gs, wave * 32 + (lane & 31), 2 * s + half) = gf[s];
+    for (int s = 0; s < Tile<T, D>::NS; ++s) *Tile<T, D>::at(Gs, row_blk * 32 + (lane & 31), 2 * s + half) = gf[s];
   }
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
 
@@ -826,16 +853,17 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_q
     const int count = make_list(list, take, t, lo, hi, tid);
     kv.start(list, count, tid);
     for (int i = 0; i < count; ++i) {
-      const int k0 = list.tile[i] * KT;
       kv.next(i, list, count, tid);
-      const int state = tile_state(a, ws, k0, KT, list.lo[i], list.hi[i]);
+      const int k0 = __builtin_amdgcn_readfirstlane(list.tile[i]) * KT;
+      const int state = tile_state(a, ws, k0, KT, __builtin_amdgcn_readfirstlane(list.lo[i]), __builtin_amdgcn_readfirstlane(list.hi[i]));
       if (state == 0) continue;
-#pragma unroll Q::SPARE ? 1 : KT / 32
-      for (int kb = 0; kb < KT / 32; ++kb) {
-        f32x16_t s = dot_rows<T, D>(kv.keys(i), 32 * kb, qf, ln), dp;
-        if constexpr (Q::SPARE) dp = dot_tiles<T, D>(kv.values(i), 32 * kb, lds_addr(Gs) + wave * 32 * Tile<T, D>::ROWB, ln);
-        else dp = dot_rows<T, D>(kv.values(i), 32 * kb, gf, ln);
-        scores<CAP, SLOPES, true>(a, sc, r, kv.ids(i) + 32 * kb, k0 + 32 * kb, half, state == 1, s, damp);
+#pragma unroll Q::SPARE ? 1 : NK
+      for (int kb = 0; kb < NK; ++kb) {
+        const int row0 = 32 * (FEW ? wave : kb);
+        f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln), dp;
+        if constexpr (Q::SPARE) dp = dot_tiles<T, D>(kv.values(i), row0, lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln);
+        else dp = dot_rows<T, D>(kv.values(i), row0, gf, ln);
+        scores<CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, half, state == 1, s, damp);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
@@ -847,10 +875,23 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_q
           s[j] = p;
           dp[j] = ds;
         }
-        if constexpr (MEND) add_outer2<T, D>(dq, pk, kv.keys(i), 32 * kb, dp, s, ln);
-        else add_outer<T, D>(dq, kv.keys(i), 32 * kb, dp, ln);
+        if constexpr (MEND) add_outer2<T, D>(dq, pk, kv.keys(i), row0, dp, s, ln);
+        else add_outer<T, D>(dq, kv.keys(i), row0, dp, ln);
       }
     }
+  }
+  if constexpr (FEW) {
+    // the sums of the other wavefronts' keys onto the first's, through the tiles' room
+    float* const rest_s = reinterpret_cast<float*>(lds + 3 * 32 * D * 4);
+    add_parts<D, 4, 1>(dq, lds, part, 0, lane);
+    if constexpr (MEND) {
+      add_parts<D, 4, 1>(pk, lds, part, 0, lane);
+      __syncthreads();
+      if (part) rest_s[(part - 1) * 64 + lane] = rest;
+      __syncthreads();
+      if (part == 0) rest = ((rest + rest_s[lane]) + rest_s[64 + lane]) + rest_s[128 + lane];
+    }
+    if (part) return;
   }
   if constexpr (MEND) {
     rest += __shfl_xor(rest, 32, 64);
@@ -866,44 +907,47 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_q
 }
 
 // ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
-// 128 keys, over tiles of the 64 / G queries whose rows fit 64 (G: heads of the group).  NW = 4: 32 keys to a wavefront.  NW = 8
-// (bf16 at width 128): two wavefronts share 32 keys, one takes the first 32 rows of a tile and one the others, and they add
-// up at the end; the values stay in LDS, as the accumulators and the keys fill the registers.
+// BLOCKS times 32 keys, over tiles of as many queries as have their rows (one for each of the G heads of the group) in RT.
+// BLOCKS wavefronts take 32 keys each; where there are more, they share the rows of a tile and add up at the end:
+//   4 of 4: 128 keys, tiles of 64 rows.  4 of 8 (bf16 at width 128): the same, two wavefronts to 32 keys; the values stay in LDS, as
+//   the accumulators and the keys fill the registers.  1 of 4 (few keys in all): 32 keys, tiles of 128 rows.
 // Few workgroups: the rows are split over a.row_splits workgroups, whose sums k_forms_kv_join adds.
-struct RowMeta {
-  float l2[64], delta[64], slope[64];
-  int lim[64], id[64], pos[64];
-};
-template <typename T, int D, int NW>
+template <typename T, int D, int BLOCKS, int NW>
 struct BwdKv {
-  static constexpr int RT = 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
+  static constexpr int PARTS = NW / BLOCKS, RT = PARTS == 4 ? 128 : 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
+  static constexpr int BUFS = TILE > 32768 ? 1 : 2;
   static constexpr bool SPARE = NW == 8;
-  static constexpr int LDS = 2 * STAGE + (SPARE ? 128 * Tile<T, D>::ROWB : 0);
+  static constexpr int LDS = BUFS * STAGE + (SPARE ? 128 * Tile<T, D>::ROWB : 0);
+  struct Meta {
+    float l2[RT], delta[RT], slope[RT];
+    int lim[RT], id[RT], pos[RT];
+  };
+  static_assert(BUFS * STAGE >= (PARTS - 1) * BLOCKS * 32 * D * 4, "the sums' room");
 };
-template <typename T, int D, bool CAP, bool SLOPES, int NW>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
-  using K = BwdKv<T, D, NW>;
-  constexpr int RT = K::RT, TILE = K::TILE, NR = NW == 8 ? 1 : 2;      // blocks of 32 rows of a tile that a wavefront takes
+template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8) ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
+  using K = BwdKv<T, D, BLOCKS, NW>;
+  constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;      // NR: blocks of 32 rows of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
-  __shared__ __attribute__((aligned(16))) RowMeta meta[2];
-  unsigned char* const Vs = lds + 2 * K::STAGE;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, blk = wave & 3, part = wave >> 2;
-  const int G = a.nh / a.nkv, QT = RT / G, used = QT * G, n_kt = (a.S + 127) / 128, first = a.S - a.n;
+  __shared__ __attribute__((aligned(16))) typename K::Meta meta[K::BUFS];
+  unsigned char* const Vs = lds + K::BUFS * K::STAGE;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, blk = wave % BLOCKS, part = wave / BLOCKS;
+  const int G = a.nh / a.nkv, QT = RT / G, used = QT * G, n_kt = (a.S + KEYS - 1) / KEYS, first = a.S - a.n;
   int bh, at;
   tile_order(blockIdx.x, a.B * a.nkv, n_kt * a.row_splits, a.causal, bh, at);     // (the first keys have the most rows)
   const int kt = at / a.row_splits, split = at % a.row_splits;
   const int hk = bh % a.nkv, b = bh / a.nkv;
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
-  const int kw = kt * 128 + blk * 32, key = kw + (lane & 31);      // this wavefront's keys, this lane's
+  const int kw = kt * KEYS + blk * 32, key = kw + (lane & 31);      // this wavefront's keys, this lane's
   const bool in = key < a.S;
   const int kid = docs ? (in ? docs[key] : -1) : 0;
   const bool live = in && kid >= 0;
   const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
   const Score sc = make_score(a.scale, a.cap);
   int klo, khi;
-  positions_range(a, b, kt * 128, min(a.S, kt * 128 + 128) - 1, klo, khi);
+  positions_range(a, b, kt * KEYS, min(a.S, kt * KEYS + KEYS) - 1, klo, khi);
 
   Frags<T, D> kf, vf;
   load_frags<T, D>(kf, head_ptr<T>(a.k, b, hk) + (long long)(in ? key : 0) * a.k.sr, half, a.w, live);
@@ -923,8 +967,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_k
   gl.init(tid, a.g.sr * (int)sizeof(T), G, a.g.sh * (int)sizeof(T), used, a.w);
   const T* qbase = head_ptr<T>(a.q, b, hk * G);
   const T* gbase = head_ptr<T>(a.g, b, hk * G);
-  auto tiles = [&](int i) { return lds + (i & 1) * K::STAGE; };
-  // queries q0 .. q0 + QT - 1 of all heads of the group; what the mask needs of a row waits in the registers of wavefront 0
+  auto tiles = [&](int i) { return lds + (K::BUFS > 1 ? (i & 1) * K::STAGE : 0); };
+  // queries q0 .. q0 + QT - 1 of all heads of the group; what the mask needs of a row waits in the registers of a thread each
   RowOf mr;
   float ml2 = 0.f, mdelta = 0.f;
   auto issue = [&](int i, int q0, int lo) {
@@ -942,7 +986,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_k
   };
   auto commit = [&](int i) {
     if (tid >= RT) return;
-    RowMeta& m = meta[i & 1];
+    typename K::Meta& m = meta[i & (K::BUFS - 1)];
     m.l2[tid] = ml2 == -INFINITY ? INFINITY : ml2 * LOG2E;     // rows that see nothing: probabilities zero
     m.delta[tid] = mdelta;
     m.slope[tid] = mr.slope2;
@@ -958,26 +1002,32 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_k
     if (tid < LIST && base + tid < n_tiles) {
       const int p0 = first + t * QT, p1 = first + min(a.n, t * QT + QT) - 1;
       positions_range(a, b, p0, p1, lo, hi);
-      take = kt * 128 < key_limit(a, p1, prefix) && (!docs || (hi >= 0 && khi >= 0 && lo <= khi && hi >= klo));
+      take = kt * KEYS < key_limit(a, p1, prefix) && (!docs || (hi >= 0 && khi >= 0 && lo <= khi && hi >= klo));
     }
     const int count = make_list(list, take, t, lo, hi, tid);
-    if (count > 0) {
-      issue(0, list.tile[0] * QT, list.lo[0]);
+    auto fetch = [&](int i) { issue(i, __builtin_amdgcn_readfirstlane(list.tile[i]) * QT, __builtin_amdgcn_readfirstlane(list.lo[i])); };
+    if (K::BUFS > 1 && count > 0) {
+      fetch(0);
       commit(0);
     }
     for (int i = 0; i < count; ++i) {
-      const int q0 = list.tile[i] * QT, p0 = first + q0, p1 = first + min(a.n, q0 + QT) - 1;
-      const int lo_t = list.lo[i], hi_t = list.hi[i];
+      const int q0 = __builtin_amdgcn_readfirstlane(list.tile[i]) * QT, p0 = first + q0, p1 = first + min(a.n, q0 + QT) - 1;
+      const int lo_t = __builtin_amdgcn_readfirstlane(list.lo[i]), hi_t = __builtin_amdgcn_readfirstlane(list.hi[i]);
+      if constexpr (K::BUFS == 1) {
+        __syncthreads();
+        fetch(i);
+        commit(i);
+      }
       __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): what commit() wrote
       landed<0, 2>(0);
-      if (i + 1 < count) issue(i + 1, list.tile[i + 1] * QT, list.lo[i + 1]);
-      const RowMeta& m = meta[i & 1];
+      if (K::BUFS > 1 && i + 1 < count) fetch(i + 1);
+      const typename K::Meta& m = meta[i & (K::BUFS - 1)];
       const uint32_t tile = lds_addr(tiles(i));
       const bool hidden = kw >= key_limit(a, p1, prefix) || kid_hi < 0 || (docs && (hi_t < kid_lo || lo_t > kid_hi));
       const bool mask = kw + 32 > key_limit(a, p0, prefix) || (docs && !(lo_t == hi_t && lo_t == kid_lo && lo_t == kid_hi));
       if (!hidden) {
 #pragma unroll 1
-        for (int rb = NR == 1 ? part : 0; rb < (NR == 1 ? part + 1 : 2); ++rb) {
+        for (int rb = part * NR; rb < part * NR + NR; ++rb) {
           f32x16_t s = dot_rows<T, D>(tile, 32 * rb, kf, ln), dp;
           if constexpr (K::SPARE) dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln);
           else dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln);
@@ -1012,35 +1062,13 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 2 : 1) k_forms_bwd_k
           add_outer<T, D>(dk, tile, 32 * rb, dp, ln);
         }
       }
-      if (i + 1 < count) commit(i + 1);
+      if (K::BUFS > 1 && i + 1 < count) commit(i + 1);
     }
   }
-  if constexpr (NW == 8) {
-    // the second part's sums onto the first's: 32 keys x 128 d a wavefront, dK and then dV through the same 64 KB
-    constexpr int LD = 16 * D / 32 * 64;
-    float* const mine = reinterpret_cast<float*>(lds) + blk * LD + lane * 4;
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      f32x16_t (&acc)[D / 32] = which ? dv : dk;
-      __syncthreads();
-      if (part == 1)
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4_t*>(mine + (4 * i + g) * 256) = f32x4_t{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
-      __syncthreads();
-      if (part == 0)
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(mine + (4 * i + g) * 256);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][4 * g + j] += x[j];
-          }
-    }
-    if (part == 1) return;
+  if constexpr (K::PARTS > 1) {
+    add_parts<D, K::PARTS, BLOCKS>(dk, lds, part, blk, lane);
+    add_parts<D, K::PARTS, BLOCKS>(dv, lds, part, blk, lane);
+    if (part) return;
   }
   if (!in) return;
   if (a.row_splits > 1) {
@@ -1086,34 +1114,39 @@ inline hipError_t launch(int threads, size_t blocks, int lds, const FormArgs& a,
   return hipGetLastError();
 }
 
-// Whether 256 rows a workgroup (eight wavefronts, half the reads of the keys) leave one for every compute unit.
-bool wide_rows(bool b16, int w, size_t heads, int rows);
+// How the rows (and, backward, the keys) are dealt out: four wavefronts to 32 rows where there are few, 32 rows to each of eight
+// (width 128 in bf16) where there are many; see attention_forms_bf16.hip.
+enum RowMode { ROWS_FEW, ROWS_FOUR, ROWS_EIGHT };
+RowMode row_mode(bool wide, size_t heads, int rows);
 
 template <typename T, int D, bool CAP, bool SLOPES>
 struct Launch {
   static constexpr bool WIDE = sizeof(T) == 2 && D == 128;
   static constexpr int NW = WIDE ? 8 : 4;
-  static size_t tiles(int rows, int nw) { return ((size_t)rows + 32 * nw - 1) / (32 * nw); }
+  static size_t tiles(int rows, int per) { return ((size_t)rows + per - 1) / per; }
   static hipError_t fwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
-    const size_t heads = (size_t)a.B * a.nkv;
+    const size_t heads = (size_t)a.B * a.nkv, each = heads * a.splits;
+    const RowMode mode = row_mode(WIDE, heads, rows);
     hipError_t e;
-    if (rows <= 32) e = launch<k_forms_fwd<T, D, CAP, SLOPES, true, 4>>(256, heads * a.splits, Fwd<T, D, true, 4>::LDS, a, s);
-    else if (WIDE && wide_rows(true, a.w, heads, rows))
-      e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, NW) * a.splits, Fwd<T, D, false, NW>::LDS, a, s);
-    else e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 4) * a.splits, Fwd<T, D, false, 4>::LDS, a, s);
+    if (mode == ROWS_FEW) e = launch<k_forms_fwd<T, D, CAP, SLOPES, true, 4>>(256, each * tiles(rows, 32), Fwd<T, D, true, 4>::LDS, a, s);
+    else if (mode == ROWS_EIGHT) e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, NW>>(64 * NW, each * tiles(rows, 32 * NW), Fwd<T, D, false, NW>::LDS, a, s);
+    else e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, 4>>(256, each * tiles(rows, 128), Fwd<T, D, false, 4>::LDS, a, s);
     if (e != hipSuccess || a.splits == 1) return e;
     return launch<k_forms_join<T>>(256, (heads * rows + 3) / 4, 0, a, s);
   }
   static hipError_t bwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv;
+    const RowMode mode = row_mode(WIDE, heads, rows);
     hipError_t e;
-    if (WIDE && wide_rows(true, a.w, heads, rows))
-      e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, NW>>(64 * NW, heads * tiles(rows, NW), BwdQ<T, D, NW>::LDS, a, s);
-    else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, 4>>(256, heads * tiles(rows, 4), BwdQ<T, D, 4>::LDS, a, s);
+    if (mode == ROWS_FEW) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, true, 4>>(256, heads * tiles(rows, 32), BwdQ<T, D, true, 4>::LDS, a, s);
+    else if (mode == ROWS_EIGHT) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, 32 * NW), BwdQ<T, D, false, NW>::LDS, a, s);
+    else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
     if (e != hipSuccess) return e;
-    e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, NW>>(64 * NW, heads * ((a.S + 127) / 128) * a.row_splits, BwdKv<T, D, NW>::LDS, a, s);
+    if (row_mode(false, heads, a.S) == ROWS_FEW)
+      e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 1, 4>>(256, heads * tiles(a.S, 32) * a.row_splits, BwdKv<T, D, 1, 4>::LDS, a, s);
+    else e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 4, NW>>(64 * NW, heads * tiles(a.S, 128) * a.row_splits, BwdKv<T, D, 4, NW>::LDS, a, s);
     if (e != hipSuccess || a.row_splits == 1) return e;
     return launch<k_forms_kv_join<T>>(256, (heads * a.S * a.w / 2 + 255) / 256, 0, a, s);
   }

@@ -20,30 +20,31 @@ hipError_t form_ranges(const FormArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The keys are split only where the workgroups of whole rows leave the chip's 256 compute units short of two each.
-int form_splits(int dtype, int B, int n, int S, int nh, int nkv, int w) {
-  (void)dtype;
-  (void)w;
-  const long long rows = (long long)n * (nh / nkv);
-  const bool few = rows <= 32;
-  const long long blocks = (long long)B * nkv * (few ? 1 : (rows + 127) / 128);
-  const int tiles = few ? (S + 127) / 128 : (S + 63) / 64;
-  const long long want = (512 + blocks - 1) / blocks, most = few ? tiles : tiles / 8;
-  const long long splits = want < most ? want : most;
-  return blocks >= 256 || splits < 1 ? 1 : (int)splits;
+namespace forms {
+// 128 rows a workgroup leave 256 compute units idle below 256 of them; 256 rows a workgroup read the keys half as often.
+RowMode row_mode(bool wide, size_t heads, int rows) {
+  if (heads * (((size_t)rows + 127) / 128) < 256) return ROWS_FEW;
+  return wide && heads * ((size_t)rows / 256) >= 256 ? ROWS_EIGHT : ROWS_FOUR;
 }
+}  // namespace forms
 
-// The key side's workgroups take 128 keys each; below two for each of 256 compute units (causal: the first keys' are the longest)
-// the rows are split, as far as every part keeps eight tiles of 64.
+// The keys are split where even 32 rows a workgroup come to fewer than 256 workgroups, as far as every part keeps two tiles.
+int form_splits(int B, int n, int S, int nh, int nkv) {
+  const long long rows = (long long)n * (nh / nkv), heads = (long long)B * nkv, blocks = heads * ((rows + 31) / 32);
+  if (blocks >= 256 || forms::row_mode(false, (size_t)heads, (int)rows) != forms::ROWS_FEW) return 1;
+  const long long want = (512 + blocks - 1) / blocks, most = (S + 127) / 256;
+  const long long splits = want < most ? want : most;
+  return splits < 1 ? 1 : (int)splits;
+}
+// The key side's workgroups take 128 keys each, or 32; below two for each of 256 compute units the rows are split, as far as every
+// part keeps eight tiles (causal: the first keys have the most rows, so that one workgroup for each unit would not do).
 int form_row_splits(int B, int n, int S, int nh, int nkv) {
-  const long long blocks = (long long)B * nkv * ((S + 127) / 128), tiles = (long long)n * (nh / nkv) / 64;
+  const bool few = forms::row_mode(false, (size_t)B * nkv, S) == forms::ROWS_FEW;
+  const long long blocks = (long long)B * nkv * (few ? (S + 31) / 32 : (S + 127) / 128), tiles = (long long)n * (nh / nkv) / (few ? 128 : 64);
   const long long want = (512 + blocks - 1) / blocks, most = tiles / 8;
   const long long splits = want < most ? want : most;
   return splits < 1 ? 1 : (int)splits;
 }
-namespace forms {
-bool wide_rows(bool b16, int w, size_t heads, int rows) { return b16 && w > 64 && heads * ((size_t)rows / 256) >= 256; }
-}  // namespace forms
 
 hipError_t form_fwd_bf16(const FormArgs& a, hipStream_t s) { return forms::fwd_t<bf16>(a, s); }
 hipError_t form_bwd_bf16(const FormArgs& a, hipStream_t s) { return forms::bwd_t<bf16>(a, s); }

@@ -269,7 +269,7 @@ struct FormArgs {
   float scale = 1.f, cap = 0.f;
 };
 // Parts the forward splits the keys into.
-int form_splits(int dtype, int B, int n, int S, int nh, int nkv, int w);
+int form_splits(int B, int n, int S, int nh, int nkv);
 // Parts the key side of the backward splits the rows into.
 int form_row_splits(int B, int n, int S, int nh, int nkv);
 hipError_t form_ranges(const FormArgs& a, hipStream_t s);

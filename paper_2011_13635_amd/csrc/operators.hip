@@ -197,7 +197,7 @@ Workspace attention_layout(int precision, int batch, int queries, int keys, int 
   Workspace w{};
   const size_t rows = (size_t)batch * heads * queries;
   size_t at = up((size_t)batch * ((keys + 63) / 64) * sizeof(int2));
-  *splits = backward ? 1 : form_splits(precision, batch, queries, keys, heads, kv_heads, width);
+  *splits = backward ? 1 : form_splits(batch, queries, keys, heads, kv_heads);
   if (*splits > 1) {
     w.part = at;
     at += up(rows * *splits * width * sizeof(float));

@@ -82,6 +82,16 @@ def test_attention_against_the_definition(shape, form, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("form", [0, 5, 6])
+@pytest.mark.parametrize("shape", [(32, 128, 128, 8, 8, 64), (40, 200, 200, 8, 8, 64), (64, 256, 256, 4, 4, 128), (70, 330, 350, 8, 4, 96),
+                                   (64, 130, 130, 6, 6, 128)], ids=lambda s: "x".join(map(str, s)))
+def test_batches_that_fill_the_chip(shape, form, dtype):
+    """128 rows a workgroup and more: small batches are dealt out 32 rows at a time."""
+    import torch
+    _case(torch, getattr(torch, dtype), *shape, seed=form, **FORMS[form])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("shape", [(1, 33, 16500, 1, 1, 8), (1, 2100, 2100, 8, 1, 16), (256, 1, 32900, 1, 1, 8), (1, 700, 2200, 2, 1, 64)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_more_tiles_than_one_list_holds(shape, dtype):
