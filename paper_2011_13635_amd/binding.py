@@ -226,38 +226,28 @@ def _refusal(message):
     return MsltError(MSLT_ERR_ARG, message)
 
 
-class _Place:
-    """Where a call runs: the device of its first tensor, and `stream` or that device's current one.  Inside the `with`,
-    tensors come from that stream's memory; tensors of another stream are marked as used on it."""
-
-    def __init__(self, name, stream, tensors):
-        import torch
-        if not tensors[0].is_cuda:
-            raise _refusal(f"{name}: tensors must be on a GPU")
-        index = tensors[0].device.index
-        for t in tensors:
-            if t is not None and t.device.index != index:
-                raise _refusal(f"{name}: tensors on different devices")
-        current = torch.cuda.current_stream(index)
-        self.stream, self.guard = current, None
-        if stream is not None and stream != current:
-            if stream.device.index != index:
-                raise _refusal(f"{name}: the stream is another device's")
-            self.stream = stream
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
-        if self.stream is not current or torch.cuda.current_device() != index:
-            self.guard = torch.cuda.stream(self.stream)      # (switches the device with it)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return C.c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _place(name, stream, first, *others):
+    """Where a call runs: the device of its first tensor and that device's current stream.  Returns the stream's handle, or None
+    with a context to call again in: `stream` is another one, or the device is not the current one.  Inside the context,
+    tensors come from that stream's memory; those handed in are marked as used on it."""
+    import torch
+    index = first.get_device()
+    if index < 0:
+        raise _refusal(f"{name}: tensors must be on a GPU")
+    for t in others:
+        if t is not None and t.get_device() != index:
+            raise _refusal(f"{name}: tensors on different devices")
+    if stream is None and torch.cuda.current_device() == index:
+        return torch.cuda.current_stream(index).cuda_stream, None
+    if stream is None:
+        stream = torch.cuda.current_stream(index)
+    elif stream.device.index != index:
+        raise _refusal(f"{name}: the stream is another device's")
+    else:
+        for t in (first, *others):
+            if t is not None:
+                t.record_stream(stream)
+    return None, torch.cuda.stream(stream)      # (switches the device with it)
 
 
 def _precision(name, t):
@@ -273,7 +263,7 @@ def _heads(name, what, t, like=None, shape=None):
     """A 4-D tensor [batch, rows, heads, width] as the C struct; like: must have its type."""
     if t.dim() != 4 or (shape is not None and t.shape != shape):
         raise _refusal(f"{name}: {what} must be [batch, rows, heads, width]" + (f" {tuple(shape)}" if shape is not None else "") +
-                         f", not {tuple(t.shape)}")
+                       f", not {tuple(t.shape)}")
     if like is not None and t.dtype is not like.dtype:
         raise _refusal(f"{name}: {what} is {t.dtype}, not {like.dtype}")
     sb, sr, sh, se = t.stride()
@@ -286,9 +276,9 @@ def _flat(name, what, t, dtype, *shapes):
     """Address of a contiguous tensor of one of the given shapes; None for None."""
     if t is None:
         return None
-    if t.dtype is not dtype or not t.is_contiguous() or all(t.shape != s for s in shapes):
+    if t.dtype is not dtype or not t.is_contiguous() or t.shape not in shapes:
         raise _refusal(f"{name}: {what} must be contiguous {dtype} {' or '.join(str(tuple(s)) for s in shapes)}, "
-                         f"not {t.dtype} {tuple(t.shape)}")
+                       f"not {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
@@ -310,14 +300,18 @@ def _rotary_sizes(name, q, k):
     return B, S, hq, 0 if k is None else k.shape[2], w
 
 
-def _results(name, what, given, inputs):
-    """The tensors results go to: the given ones, or new contiguous ones."""
+def _result(given, like):
+    """The tensor a result goes to: the given one, or a new contiguous one."""
     import torch
-    given = given if given is not None else (None,) * len(inputs)
-    if len(given) != len(inputs):
-        raise _refusal(f"{name}: {what} must hold {len(inputs)} tensors")
-    return [x if o is None and x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) if o is None else o
-            for o, x in zip(given, inputs)]
+    return given if given is not None else torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
+def _given(name, what, given, n):
+    if given is None:
+        return (None,) * n
+    if len(given) != n:
+        raise _refusal(f"{name}: {what} must hold {n} tensors")
+    return given
 
 
 def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None, stream=None):
@@ -326,16 +320,20 @@ def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None,
     for the results, q and k themselves allowed.  Returns them.  Enqueues only."""
     import torch
     name = "mslt_rotary"
+    oq, ok = _given(name, "out", out, 2)
+    st, place = _place(name, stream, q, k, positions, oq, ok)
+    if place is not None:
+        with place:
+            return mslt_rotary(q, k, form, positions, inverse, out)
     B, S, hq, hk, w = _rotary_sizes(name, q, k)
-    with _Place(name, stream, [q, k, positions] + list(out or ())) as st:
-        oq, ok = _results(name, "out", out, (q, k))
-        hq_in, hq_out = _heads(name, "q", q), _heads(name, "out", oq, q, q.shape)
-        hk_in = hk_out = None
-        if k is not None:
-            hk_in, hk_out = C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "out", ok, q, k.shape))
-        _check(load_library().mslt_rotary(st, _precision(name, q), B, S, hq, hk, w, C.byref(hq_in), hk_in,
-                                          _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form), int(inverse),
-                                          C.byref(hq_out), hk_out))
+    oq = _result(oq, q)
+    kin = kout = None
+    if k is not None:
+        ok = _result(ok, k)
+        kin, kout = C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "out", ok, q, k.shape))
+    _check(load_library().mslt_rotary(st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), kin,
+                                      _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form), int(inverse),
+                                      C.byref(_heads(name, "out", oq, q, q.shape)), kout))
     return oq, ok
 
 
@@ -351,13 +349,17 @@ def mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form: RotaryForm, positions
     the two results.  Enqueues only."""
     import torch
     name = "mslt_head_norm_rotary"
+    oq, ok = _given(name, "out", out, 2)
+    st, place = _place(name, stream, q, k, gain_q, gain_k, positions, oq, ok)
+    if place is not None:
+        with place:
+            return mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form, positions, out)
     B, S, hq, hk, w = _rotary_sizes(name, q, k)
-    with _Place(name, stream, [q, k, gain_q, gain_k, positions] + list(out or ())) as st:
-        oq, ok = _results(name, "out", out, (q, k))
-        _check(load_library().mslt_head_norm_rotary(
-            st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)),
-            *_gains(name, gain_q, gain_k, hq, hk, w), eps, _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
-            C.byref(_heads(name, "out", oq, q, q.shape)), C.byref(_heads(name, "out", ok, q, k.shape))))
+    oq, ok = _result(oq, q), _result(ok, k)
+    _check(load_library().mslt_head_norm_rotary(
+        st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)),
+        *_gains(name, gain_q, gain_k, hq, hk, w), eps, _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
+        C.byref(_heads(name, "out", oq, q, q.shape)), C.byref(_heads(name, "out", ok, q, k.shape))))
     return oq, ok
 
 
@@ -365,22 +367,25 @@ def mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form: RotaryForm, 
     """Gradients of mslt_head_norm_rotary from those of its results; q, k and the gains as it got them.  out: tensors for
     dq and dk, grad_q and grad_k themselves allowed.  Returns a dict of dq, dk, dgain_q, dgain_k.  Enqueues only."""
     import torch
-    name = "mslt_head_norm_rotary_backward"
+    name, lib = "mslt_head_norm_rotary_backward", load_library()
+    dq, dk = _given(name, "out", out, 2)
+    st, place = _place(name, stream, q, k, gain_q, gain_k, grad_q, grad_k, positions, dq, dk)
+    if place is not None:
+        with place:
+            return mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form, grad_q, grad_k, positions, out)
     B, S, hq, hk, w = _rotary_sizes(name, q, k)
-    lib = load_library()
-    with _Place(name, stream, [q, k, gain_q, gain_k, grad_q, grad_k, positions] + list(out or ())) as st:
-        dq, dk = _results(name, "out", out, (q, k))
-        gains = _gains(name, gain_q, gain_k, hq, hk, w)
-        dgq, dgk = torch.empty_like(gain_q), torch.empty_like(gain_k)
-        need = C.c_size_t()
-        _check(lib.mslt_head_norm_workspace(B, S, hq, hk, w, C.byref(need)))
-        ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        _check(lib.mslt_head_norm_rotary_backward(
-            st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), *gains, eps,
-            _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
-            C.byref(_heads(name, "grad_q", grad_q, q, q.shape)), C.byref(_heads(name, "grad_k", grad_k, q, k.shape)),
-            C.byref(_heads(name, "out", dq, q, q.shape)), C.byref(_heads(name, "out", dk, q, k.shape)),
-            dgq.data_ptr(), dgk.data_ptr(), ws.data_ptr(), need.value))
+    gains = _gains(name, gain_q, gain_k, hq, hk, w)
+    dq, dk = _result(dq, q), _result(dk, k)
+    dgq, dgk = torch.empty_like(gain_q), torch.empty_like(gain_k)
+    need = C.c_size_t()
+    _check(lib.mslt_head_norm_workspace(B, S, hq, hk, w, C.byref(need)))
+    ws = gain_q.new_empty(need.value // 4 + 1)
+    _check(lib.mslt_head_norm_rotary_backward(
+        st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), *gains, eps,
+        _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
+        C.byref(_heads(name, "grad_q", grad_q, q, q.shape)), C.byref(_heads(name, "grad_k", grad_k, q, k.shape)),
+        C.byref(_heads(name, "out", dq, q, q.shape)), C.byref(_heads(name, "out", dk, q, k.shape)),
+        dgq.data_ptr(), dgk.data_ptr(), ws.data_ptr(), need.value))
     return {"dq": dq, "dk": dk, "dgain_q": dgq, "dgain_k": dgk}
 
 
@@ -403,11 +408,10 @@ def _attention_call(name, q, k, v, form, documents, prefix, slopes):
             (C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "v", v, q, k.shape))), f)
 
 
-def _attention_workspace(lib, sizes, backward, device):
-    import torch
+def _attention_workspace(lib, sizes, backward, lse):
     need = C.c_size_t()
     _check(lib.mslt_attention_workspace(*sizes, backward, C.byref(need)))
-    return torch.empty(need.value, dtype=torch.uint8, device=device)
+    return lse.new_empty(need.value // 4 + 1), need.value
 
 
 def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, slopes=None, out=None, stream=None):
@@ -416,13 +420,16 @@ def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, sl
     slopes: fp32 [heads].  out: tensor for the result.  Returns a dict of out and lse.  Enqueues only."""
     import torch
     name, lib = "mslt_attention", load_library()
-    with _Place(name, stream, [q, k, v, documents, prefix, slopes, out]) as st:
-        sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
-        out, = _results(name, "out", (out,), (q,))
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-        ws = _attention_workspace(lib, sizes, 0, q.device)
-        _check(lib.mslt_attention(st, *sizes, *qkv, C.byref(f), C.byref(_heads(name, "out", out, q, q.shape)), lse.data_ptr(),
-                                  ws.data_ptr(), ws.numel()))
+    st, place = _place(name, stream, q, k, v, documents, prefix, slopes, out)
+    if place is not None:
+        with place:
+            return mslt_attention(q, k, v, form, documents, prefix, slopes, out)
+    sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
+    out = _result(out, q)
+    lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32)
+    ws, room = _attention_workspace(lib, sizes, 0, lse)
+    _check(lib.mslt_attention(st, *sizes, *qkv, C.byref(f), C.byref(_heads(name, "out", out, q, q.shape)), lse.data_ptr(),
+                              ws.data_ptr(), room))
     return {"out": out, "lse": lse}
 
 
@@ -432,15 +439,19 @@ def mslt_attention_backward(q, k, v, out, lse, grad_out, form: AttentionForm, do
     and dv.  Returns a dict of dq, dk, dv.  Enqueues only."""
     import torch
     name, lib = "mslt_attention_backward", load_library()
-    with _Place(name, stream, [q, k, v, out, lse, grad_out, documents, prefix, slopes] + list(grads or ())) as st:
-        sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
-        dq, dk, dv = _results(name, "grads", grads, (q, k, v))
-        ws = _attention_workspace(lib, sizes, 1, q.device)
-        _check(lib.mslt_attention_backward(
-            st, *sizes, *qkv, C.byref(_heads(name, "out", out, q, q.shape)),
-            _flat(name, "lse", lse, torch.float32, (q.shape[0], q.shape[2], q.shape[1])),
-            C.byref(_heads(name, "grad_out", grad_out, q, q.shape)), C.byref(f), C.byref(_heads(name, "grads", dq, q, q.shape)),
-            C.byref(_heads(name, "grads", dk, q, k.shape)), C.byref(_heads(name, "grads", dv, q, k.shape)), ws.data_ptr(), ws.numel()))
+    dq, dk, dv = _given(name, "grads", grads, 3)
+    st, place = _place(name, stream, q, k, v, out, lse, grad_out, documents, prefix, slopes, dq, dk, dv)
+    if place is not None:
+        with place:
+            return mslt_attention_backward(q, k, v, out, lse, grad_out, form, documents, prefix, slopes, grads)
+    sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
+    dq, dk, dv = _result(dq, q), _result(dk, k), _result(dv, v)
+    ws, room = _attention_workspace(lib, sizes, 1, lse)
+    _check(lib.mslt_attention_backward(
+        st, *sizes, *qkv, C.byref(_heads(name, "out", out, q, q.shape)),
+        _flat(name, "lse", lse, torch.float32, (q.shape[0], q.shape[2], q.shape[1])),
+        C.byref(_heads(name, "grad_out", grad_out, q, q.shape)), C.byref(f), C.byref(_heads(name, "grads", dq, q, q.shape)),
+        C.byref(_heads(name, "grads", dk, q, k.shape)), C.byref(_heads(name, "grads", dv, q, k.shape)), ws.data_ptr(), room))
     return {"dq": dq, "dk": dk, "dv": dv}
 
 

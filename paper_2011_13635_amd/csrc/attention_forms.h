@@ -12,7 +12,7 @@
 // out of the same LDS tile that the first product reads by rows.
 //
 // Which tiles a workgroup visits: tiles that no row of it can see are left out.  For documents, the least and largest
-// entry of every 64 positions are found first (k_doc_ranges); each workgroup turns them and the position limits into a
+// entry of every 64 positions are found first (doc_ranges); each workgroup turns them and the position limits into a
 // list of tiles.  A wavefront masks element by element only in tiles that are neither hidden from all its rows nor open
 // to all of them.
 #pragma once
@@ -211,7 +211,20 @@ __device__ __forceinline__ Score make_score(float scale, float cap) {
   return cap > 0.f ? Score{2.f * LOG2E * scale / cap, cap * LOG2E} : Score{scale * LOG2E, 0.f};
 }
 
-__device__ __forceinline__ const int2* range_row(const FormArgs& a, int b) { return a.ranges + (size_t)b * ((a.S + 63) / 64); }
+// Least and largest document entry of every 64 positions of a sequence.  Up to 64 such blocks a workgroup finds them itself, one
+// wavefront a block (a launch of its own takes longer); beyond that k_doc_ranges has.  Called by the whole workgroup.
+__device__ __forceinline__ const int2* doc_ranges(const FormArgs& a, int b, int2 (&room)[FORM_OWN_RANGES], int tid, int threads) {
+  const int blocks = (a.S + 63) / 64;
+  if (!a.docs) return nullptr;
+  if (blocks > FORM_OWN_RANGES) return a.ranges + (size_t)b * blocks;
+  for (int i = tid >> 6; i < blocks; i += threads >> 6) {
+    const int v = a.docs[(size_t)b * a.S + min(64 * i + (tid & 63), a.S - 1)];
+    const int lo = wave_min_i(v), hi = wave_max_i(v);
+    if ((tid & 63) == 0) room[i] = make_int2(lo, hi);
+  }
+  __syncthreads();
+  return room;
+}
 
 // Which tile of which kv head a workgroup takes.  Workgroups go round the eight XCDs; the tiles of one kv head are given to one
 // XCD, or to 8 / heads of them when there are fewer heads, so that its keys and values stay in few L2s.  uneven (causal): tiles
@@ -438,10 +451,9 @@ __device__ __forceinline__ int tile_state(const FormArgs& a, const Span& s, int 
   return a.docs && !(lo == hi && lo == s.id_lo && lo == s.id_hi) ? 1 : 2;
 }
 // least and largest document entry of the positions p0 .. p1, by whole blocks of 64 of them
-__device__ __forceinline__ void positions_range(const FormArgs& a, int b, int p0, int p1, int& lo, int& hi) {
+__device__ __forceinline__ void positions_range(const int2* r, int p0, int p1, int& lo, int& hi) {
   lo = hi = 0;
-  if (!a.docs) return;
-  const int2* r = range_row(a, b);
+  if (!r) return;
   lo = 0x7fffffff;
   hi = -0x7fffffff;
   for (int i = p0 >> 6; i <= p1 >> 6; ++i) {
@@ -578,6 +590,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_
   constexpr int NK = FEW ? 1 : F::KT / 32;       // blocks of 32 keys of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
+  __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ int span_s[NW][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + F::ROWS - 1) / F::ROWS;
@@ -587,6 +600,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_
   const int hk = bh % a.nkv, b = bh / a.nkv;
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
   const RowOf r = row_of(a, rt * F::ROWS + (FEW ? 0 : wave * 32) + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
   Frags<T, D> qf;
@@ -628,7 +642,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_
     const int t = base + tid;
     int lo = 0, hi = 0, take = 0;
     if (tid < LIST && t < t_end) {
-      positions_range(a, b, t * F::KT, min(a.S, (t + 1) * F::KT) - 1, lo, hi);
+      positions_range(ranges, t * F::KT, min(a.S, (t + 1) * F::KT) - 1, lo, hi);
       take = tile_state(a, gs, t * F::KT, F::KT, lo, hi) != 0;
     }
     const int count = make_list(list, take, t, lo, hi, tid);
@@ -799,6 +813,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   constexpr bool MEND = Q::MEND;
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
+  __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ int span_s[NW][4];
   unsigned char* const Gs = lds + Q::Keys::LDS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, part = FEW ? wave : 0, row_blk = FEW ? 0 : wave;
@@ -808,6 +823,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const int rt = a.causal ? n_rt - 1 - at : at, hk = bh % a.nkv, b = bh / a.nkv;
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
   const RowOf r = row_of(a, rt * Q::ROWS + row_blk * 32 + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
   const Score sc = make_score(a.scale, a.cap);
@@ -847,7 +863,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
     const int t = base + tid;
     int lo = 0, hi = 0, take = 0;
     if (tid < LIST && t < n_tiles) {
-      positions_range(a, b, t * KT, min(a.S, (t + 1) * KT) - 1, lo, hi);
+      positions_range(ranges, t * KT, min(a.S, (t + 1) * KT) - 1, lo, hi);
       take = tile_state(a, gs, t * KT, KT, lo, hi) != 0;
     }
     const int count = make_list(list, take, t, lo, hi, tid);
@@ -930,6 +946,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;      // NR: blocks of 32 rows of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
+  __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ __attribute__((aligned(16))) typename K::Meta meta[K::BUFS];
   unsigned char* const Vs = lds + K::BUFS * K::STAGE;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, blk = wave % BLOCKS, part = wave / BLOCKS;
@@ -946,8 +963,9 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const bool live = in && kid >= 0;
   const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
   const Score sc = make_score(a.scale, a.cap);
+  const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
   int klo, khi;
-  positions_range(a, b, kt * KEYS, min(a.S, kt * KEYS + KEYS) - 1, klo, khi);
+  positions_range(ranges, kt * KEYS, min(a.S, kt * KEYS + KEYS) - 1, klo, khi);
 
   Frags<T, D> kf, vf;
   load_frags<T, D>(kf, head_ptr<T>(a.k, b, hk) + (long long)(in ? key : 0) * a.k.sr, half, a.w, live);
@@ -1001,7 +1019,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
     int lo = 0, hi = 0, take = 0;
     if (tid < LIST && base + tid < n_tiles) {
       const int p0 = first + t * QT, p1 = first + min(a.n, t * QT + QT) - 1;
-      positions_range(a, b, p0, p1, lo, hi);
+      positions_range(ranges, p0, p1, lo, hi);
       take = kt * KEYS < key_limit(a, p1, prefix) && (!docs || (hi >= 0 && khi >= 0 && lo <= khi && hi >= klo));
     }
     const int count = make_list(list, take, t, lo, hi, tid);

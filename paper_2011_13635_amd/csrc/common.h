@@ -261,13 +261,14 @@ struct FormArgs {
   const int32_t* docs = nullptr;         // [B, S] or null
   const int32_t* prefix = nullptr;       // [B] or null
   const float* slopes = nullptr;         // [nh] or null
-  int2* ranges = nullptr;                // scratch [B, ceil(S / 64)]: least and largest of docs in each 64 positions
+  int2* ranges = nullptr;                // scratch [B, ceil(S / 64)]: least and largest of docs in each 64 positions (longer ones)
   float* part = nullptr;                 // scratch of split keys: [splits, B, nkv, rows, w], and maximum and sum; of split rows
                                          // (backward): [row_splits, dk then dv, B, nkv, S, w]
   float2* part_ml = nullptr;
   int B = 0, n = 0, S = 0, nh = 0, nkv = 0, w = 0, causal = 0, splits = 1, row_splits = 1;
   float scale = 1.f, cap = 0.f;
 };
+constexpr int FORM_OWN_RANGES = 64;      // blocks of 64 positions whose documents a workgroup looks at itself
 // Parts the forward splits the keys into.
 int form_splits(int B, int n, int S, int nh, int nkv);
 // Parts the key side of the backward splits the rows into.

@@ -65,19 +65,19 @@ static int rotary_form(const char* who, const mslt_rotary_form* f, int width, Ro
   a.interleaved = f->interleaved != 0;
   a.magnitude = f->magnitude;
   // theta^(-2i/r) as products of one ratio: r/2 factors, each rounding 2^-64 of the value
-  const long double tau = 6.283185307179586476925286766559L;
+  const long double turns = 0.159154943091895335768883763372514362L;      // 1 / 2pi
   const long double ratio = r ? powl((long double)f->theta, -2.0L / r) : 1.0L;
   long double freq = 1.0L;
   for (int i = 0; i < a.pairs; ++i, freq *= ratio) {
     long double x = freq;
     if (f->scaling == 1) x = freq / f->factor;
     if (f->scaling == 2) {
-      long double t = ((long double)f->original_length * freq / tau - f->low_turns) / ((long double)f->high_turns - f->low_turns);
+      long double t = ((long double)f->original_length * freq * turns - f->low_turns) / ((long double)f->high_turns - f->low_turns);
       t = t < 0.0L ? 0.0L : t > 1.0L ? 1.0L : t;
       x = freq * (t + (1.0L - t) / f->factor);
     }
-    x /= tau;
-    x -= floorl(x);          // whole turns per position turn nothing
+    x *= turns;
+    if (x >= 1.0L) x -= floorl(x);          // whole turns per position turn nothing
     const long double units = x * 18446744073709551616.0L + 0.5L;
     a.freq[i] = units >= 18446744073709551616.0L ? 0ull : (unsigned long long)units;
   }
