@@ -43,15 +43,23 @@ __device__ __forceinline__ f32x16_t zero16() {
 }
 // row of a 32-row block that register r of this half-wave holds, without the 4 * half
 __device__ __forceinline__ constexpr int acc_row(int r) { return 8 * (r >> 2) + (r & 3); }
+// Least and largest of the 64 lanes' values, by moves between neighbouring lanes (a shuffle through LDS takes some 70 cycles, a move
+// eight): within four, rows of sixteen, then across the rows; lane 63 holds the result.
+template <typename F>
+__device__ __forceinline__ int wave_reduce_i(int v, F f) {
+  v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x111, 0xf, 0xf, false));     // row_shr:1, 2, 4, 8
+  v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x112, 0xf, 0xf, false));
+  v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x114, 0xf, 0xf, false));
+  v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x118, 0xf, 0xf, false));
+  v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x142, 0xa, 0xf, false));     // row_bcast:15, 31
+  v = f(v, __builtin_amdgcn_update_dpp(v, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ __forceinline__ int wave_min_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
+  return wave_reduce_i(v, [](int x, int y) { return min(x, y); });
 }
 __device__ __forceinline__ int wave_max_i(int v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
+  return wave_reduce_i(v, [](int x, int y) { return max(x, y); });
 }
 
 // LDS tile of rows of D elements in 16-byte chunks; chunk c of a row sits in place c ^ swz(row).  The order makes both
@@ -195,11 +203,23 @@ __device__ __forceinline__ void add_outer2(f32x16_t (&x)[D / 32], f32x16_t (&y)[
   }
 }
 
-// Score in base 2 from the product of a query and a key, and what the gradient is multiplied by behind the cap.
-// tanh x = 1 - 2 / (1 + e^2x): absolute error a few 2^-24 for any x, and the score's is cap times that.
+// Score in base 2 from the product x of a query and a key, and what the gradient is multiplied by behind the cap.
+// tanh y = 1 - 2 / (1 + e^2y): absolute error a few 2^-24 for any y, and the score's is cap times that.  bf16, scores within six
+// tenths of the cap: y (c0 + c1 y^2 + c2 y^4 + c3 y^6) fitted to the least largest error, 5.9e-7, five multiply-adds in place of
+// two transcendental instructions (8.4 cycles each against 3) and three more.
 struct Score {
-  float a, c;      // no cap: s2 = a * x.  cap: s2 = c * tanh, exponent a * x
+  float a, c;              // no cap: s2 = a x.  cap: s2 = c tanh, exponent a x
+  float p[4], reach;       // s2 = x (p0 + p1 x^2 + ...) for |x| <= reach
 };
+template <bool CAP>
+__device__ __forceinline__ Score make_score(float scale, float cap) {
+  Score f{scale * LOG2E, 0.f, {0.f, 0.f, 0.f, 0.f}, 0.f};
+  if constexpr (CAP) {
+    const float y = scale / cap, u = y * y, c = cap * LOG2E;
+    f = Score{2.f * LOG2E * y, c, {c * y * 0.99999102f, c * y * u * -0.33298975f, c * y * u * u * 0.1297456f, c * y * u * u * u * -0.03961138f}, 0.6f / y};
+  }
+  return f;
+}
 template <bool CAP>
 __device__ __forceinline__ float score2(const Score& f, float x, float& damp) {
   if constexpr (!CAP) return f.a * x;
@@ -207,8 +227,30 @@ __device__ __forceinline__ float score2(const Score& f, float x, float& damp) {
   damp = fmaf(-t, t, 1.f);
   return f.c * t;
 }
-__device__ __forceinline__ Score make_score(float scale, float cap) {
-  return cap > 0.f ? Score{2.f * LOG2E * scale / cap, cap * LOG2E} : Score{scale * LOG2E, 0.f};
+// the same for 16 scores at once
+template <typename T, bool DAMP>
+__device__ __forceinline__ void cap_scores(const Score& f, f32x16_t& s, f32x16_t& damp) {
+  if constexpr (sizeof(T) == 2) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(s[i]));
+    if (!__any(!(top <= f.reach))) {
+      const float ic2 = 1.f / (f.c * f.c);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float u = s[i] * s[i];
+        s[i] *= fmaf(u, fmaf(u, fmaf(u, f.p[3], f.p[2]), f.p[1]), f.p[0]);
+        if constexpr (DAMP) damp[i] = fmaf(-ic2 * s[i], s[i], 1.f);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float d = 1.f;
+    s[i] = score2<true>(f, s[i], d);
+    if constexpr (DAMP) damp[i] = d;
+  }
 }
 
 // Least and largest document entry of every 64 positions of a sequence.  Up to 64 such blocks a workgroup finds them itself, one
@@ -416,30 +458,46 @@ __device__ __forceinline__ RowOf row_of(const FormArgs& a, int R, int b, int hk,
   r.slope2 = a.slopes ? a.slopes[r.head] * LOG2E : 0.f;
   return r;
 }
-// Limits and document entries of the live rows of a wavefront, or of a workgroup.
+// Limits and document entries of the live rows among R0 .. R0 + count - 1.  Limits grow with the position: the first and the last
+// row inside the tensor bound them.
 struct Span {
   int lim_lo, lim_hi, id_lo, id_hi;
 };
-__device__ __forceinline__ Span wave_span(const RowOf& r) {
-  constexpr int BIG = 0x7fffffff;
-  return Span{wave_min_i(r.live ? r.lim : BIG), wave_max_i(r.lim), wave_min_i(r.live ? r.id : BIG), wave_max_i(r.live ? r.id : -1)};
+__device__ __forceinline__ void span_limits(const FormArgs& a, Span& s, int R0, int count, int prefix) {
+  const int G = a.nh / a.nkv, rows = a.n * G, first = a.S - a.n;
+  s.lim_lo = 0x7fffffff;
+  s.lim_hi = 0;
+  if (R0 >= rows) return;
+  s.lim_lo = key_limit(a, first + R0 / G, prefix);
+  s.lim_hi = key_limit(a, first + (min(rows, R0 + count) - 1) / G, prefix);
 }
-template <int NW>
-__device__ __forceinline__ Span group_span(const Span& w, int (&shared)[NW][4], int wave, int lane) {
-  if (lane == 0) {
-    shared[wave][0] = w.lim_lo;
-    shared[wave][1] = w.lim_hi;
-    shared[wave][2] = w.id_lo;
-    shared[wave][3] = w.id_hi;
+__device__ __forceinline__ Span wave_span(const FormArgs& a, const RowOf& r, int R0, int prefix) {
+  Span s{0, 0, 0, 0};
+  span_limits(a, s, R0, 32, prefix);
+  if (a.docs) {
+    s.id_lo = wave_min_i(r.live ? r.id : 0x7fffffff);
+    s.id_hi = wave_max_i(r.live ? r.id : -1);
+    if (s.id_hi < 0) s.lim_hi = 0;
   }
-  __syncthreads();
+  return s;
+}
+// of the whole workgroup, whose rows start at R0
+template <int NW>
+__device__ __forceinline__ Span group_span(const FormArgs& a, const Span& w, int (&shared)[NW][2], int R0, int count, int prefix, int wave, int lane) {
   Span s = w;
+  span_limits(a, s, R0, count, prefix);
+  if (a.docs) {
+    if (lane == 0) {
+      shared[wave][0] = w.id_lo;
+      shared[wave][1] = w.id_hi;
+    }
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NW; ++i) {
-    s.lim_lo = min(s.lim_lo, shared[i][0]);
-    s.lim_hi = max(s.lim_hi, shared[i][1]);
-    s.id_lo = min(s.id_lo, shared[i][2]);
-    s.id_hi = max(s.id_hi, shared[i][3]);
+    for (int i = 0; i < NW; ++i) {
+      s.id_lo = min(s.id_lo, __builtin_amdgcn_readfirstlane(shared[i][0]));
+      s.id_hi = max(s.id_hi, __builtin_amdgcn_readfirstlane(shared[i][1]));
+    }
+    if (s.id_hi < 0) s.lim_hi = 0;
   }
   return s;
 }
@@ -466,27 +524,22 @@ __device__ __forceinline__ void positions_range(const int2* r, int p0, int p1, i
 // score_factor() is the score in base 2; without cap and distance that leaves the factor to the exponential's own multiply-add.
 template <bool CAP, bool SLOPES>
 __device__ __forceinline__ float score_factor(const Score& f) { return CAP || SLOPES ? 1.f : f.a; }
-template <bool CAP, bool SLOPES, bool DAMP>
+template <typename T, bool CAP, bool SLOPES, bool DAMP>
 __device__ __forceinline__ void open_scores(const Score& f, const RowOf& r, int k0, int half, f32x16_t& s, f32x16_t& damp) {
-  if constexpr (CAP) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float d = 1.f;
-      s[i] = score2<CAP>(f, s[i], d);
-      if constexpr (DAMP) damp[i] = d;
-    }
-  }
+  if constexpr (CAP) cap_scores<T, DAMP>(f, s, damp);
   if constexpr (SLOPES) {
     const float far = (float)(r.pos - k0 - 4 * half), c = CAP ? 1.f : f.a;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope2, fabsf(far - (float)acc_row(i)), c * s[i]);
   }
 }
-// the keys that the row does not see get -infinity
-__device__ __forceinline__ void hide(const FormArgs& a, const RowOf& r, const int* ids, int k0, int half, f32x16_t& s) {
-  const int lim = r.lim - k0 - 4 * half;
+// the keys that the row does not see get -infinity; limit: the least of the wavefront's rows
+__device__ __forceinline__ void hide(const FormArgs& a, const RowOf& r, const int* ids, int k0, int limit, int half, f32x16_t& s) {
+  if (k0 + 32 > limit) {
+    const int lim = r.lim - k0 - 4 * half;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s[i] = acc_row(i) < lim ? s[i] : -INFINITY;
+    for (int i = 0; i < 16; ++i) s[i] = acc_row(i) < lim ? s[i] : -INFINITY;
+  }
   if (a.docs) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -497,11 +550,11 @@ __device__ __forceinline__ void hide(const FormArgs& a, const RowOf& r, const in
     }
   }
 }
-template <bool CAP, bool SLOPES, bool DAMP>
-__device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int half, bool mask,
+template <typename T, bool CAP, bool SLOPES, bool DAMP>
+__device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int limit, int half, bool mask,
                                        f32x16_t& s, f32x16_t& damp) {
-  open_scores<CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
-  if (mask) hide(a, r, ids, k0, half, s);
+  open_scores<T, CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
+  if (mask) hide(a, r, ids, k0, limit, half, s);
 }
 
 // Tiles of keys and values in STAGES stages: while one is worked on, the loads of the next ones are on their way.
@@ -560,11 +613,11 @@ struct KeyTiles {
 // FEW = false: 32 rows to each of NW wavefronts.  FEW = true (few rows in all): four wavefronts share 32 rows, each takes 32 keys of
 // a tile of 128, and they join their results in LDS at the end.
 // Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
-template <typename T, int D, bool FEW, int NW>
+template <typename T, int D, bool CAP, bool FEW, int NW>
 struct Fwd {
   static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB, STAGES = TILE > 32768 ? 1 : 2;
   // wavefronts that share a SIMD: as many as the registers of the accumulators allow
-  static constexpr int WAVES = sizeof(T) == 4 ? 1 : D == 64 && !FEW ? 4 : 2;
+  static constexpr int WAVES = sizeof(T) == 4 ? 1 : D == 64 && !FEW ? (CAP ? 3 : 4) : 2;
   using Keys = KeyTiles<T, D, KT, STAGES, NW>;
   static constexpr int JOIN = FEW ? 4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 : 0;
   static constexpr int LDS = Keys::LDS > JOIN ? Keys::LDS : JOIN;
@@ -584,14 +637,14 @@ __device__ __forceinline__ float row_top(const f32x16_t& s) {
 }
 
 template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
-__global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_fwd(FormArgs a) {
-  using F = Fwd<T, D, FEW, NW>;
+__global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_forms_fwd(FormArgs a) {
+  using F = Fwd<T, D, CAP, FEW, NW>;
   static_assert(!FEW || NW == 4, "the wavefronts that share 32 rows");
   constexpr int NK = FEW ? 1 : F::KT / 32;       // blocks of 32 keys of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
-  __shared__ int span_s[NW][4];
+  __shared__ int span_s[NW][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + F::ROWS - 1) / F::ROWS;
   int bh, at;
@@ -601,11 +654,12 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
-  const RowOf r = row_of(a, rt * F::ROWS + (FEW ? 0 : wave * 32) + (lane & 31), b, hk, prefix);
-  const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
+  const int R0 = rt * F::ROWS, Rw = __builtin_amdgcn_readfirstlane(R0 + (FEW ? 0 : wave * 32));
+  const RowOf r = row_of(a, Rw + (lane & 31), b, hk, prefix);
+  const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, F::ROWS, prefix, wave, lane);
   Frags<T, D> qf;
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
-  const Score sc = make_score(a.scale, a.cap);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename F::Keys kv;
@@ -661,7 +715,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, FEW, NW>::WAVES)) k_forms_
       for (int kb = 0; kb < NK; ++kb) {
         const int row0 = 32 * (kb0 + kb);
         f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln);
-        scores<CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, half, state == 1, s, unused);
+        scores<T, CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, unused);
         refer(factor * row_top(s));
         powers(s);
         add_outer<T, D>(o, kv.values(i), row0, s, ln);
@@ -814,7 +868,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
-  __shared__ int span_s[NW][4];
+  __shared__ int span_s[NW][2];
   unsigned char* const Gs = lds + Q::Keys::LDS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, part = FEW ? wave : 0, row_blk = FEW ? 0 : wave;
   const int G = a.nh / a.nkv, rows = a.n * G, n_rt = (rows + Q::ROWS - 1) / Q::ROWS;
@@ -824,9 +878,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
   const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
-  const RowOf r = row_of(a, rt * Q::ROWS + row_blk * 32 + (lane & 31), b, hk, prefix);
-  const Span ws = wave_span(r), gs = group_span<NW>(ws, span_s, wave, lane);
-  const Score sc = make_score(a.scale, a.cap);
+  const int R0 = rt * Q::ROWS, Rw = __builtin_amdgcn_readfirstlane(R0 + row_blk * 32);
+  const RowOf r = row_of(a, Rw + (lane & 31), b, hk, prefix);
+  const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, Q::ROWS, prefix, wave, lane);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename Q::Keys kv;
@@ -879,7 +934,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
         f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln), dp;
         if constexpr (Q::SPARE) dp = dot_tiles<T, D>(kv.values(i), row0, lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln);
         else dp = dot_rows<T, D>(kv.values(i), row0, gf, ln);
-        scores<CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, half, state == 1, s, damp);
+        scores<T, CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, damp);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
@@ -962,7 +1017,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const int kid = docs ? (in ? docs[key] : -1) : 0;
   const bool live = in && kid >= 0;
   const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
-  const Score sc = make_score(a.scale, a.cap);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
   const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
   int klo, khi;
   positions_range(ranges, kt * KEYS, min(a.S, kt * KEYS + KEYS) - 1, klo, khi);
@@ -1049,13 +1104,15 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
           f32x16_t s = dot_rows<T, D>(tile, 32 * rb, kf, ln), dp;
           if constexpr (K::SPARE) dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln);
           else dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln);
+          f32x16_t damp;
+          if constexpr (CAP) cap_scores<T, true>(sc, s, damp);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int at4 = 32 * rb + 8 * g + 4 * half;
             const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at4), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at4);
-            float x[4], d[4] = {1.f, 1.f, 1.f, 1.f};
+            float x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = score2<CAP>(sc, s[4 * g + j], d[j]);
+            for (int j = 0; j < 4; ++j) x[j] = CAP ? s[4 * g + j] : sc.a * s[4 * g + j];
             if constexpr (SLOPES) {
               const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
               const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
@@ -1073,7 +1130,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
             for (int j = 0; j < 4; ++j) {
               const float p = __builtin_amdgcn_exp2f(x[j] - l2[j]);
               s[4 * g + j] = p;
-              dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * d[j];
+              dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
             }
           }
           add_outer<T, D>(dv, tile + TILE, 32 * rb, s, ln);
@@ -1147,9 +1204,9 @@ struct Launch {
     const size_t heads = (size_t)a.B * a.nkv, each = heads * a.splits;
     const RowMode mode = row_mode(WIDE, heads, rows);
     hipError_t e;
-    if (mode == ROWS_FEW) e = launch<k_forms_fwd<T, D, CAP, SLOPES, true, 4>>(256, each * tiles(rows, 32), Fwd<T, D, true, 4>::LDS, a, s);
-    else if (mode == ROWS_EIGHT) e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, NW>>(64 * NW, each * tiles(rows, 32 * NW), Fwd<T, D, false, NW>::LDS, a, s);
-    else e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, 4>>(256, each * tiles(rows, 128), Fwd<T, D, false, 4>::LDS, a, s);
+    if (mode == ROWS_FEW) e = launch<k_forms_fwd<T, D, CAP, SLOPES, true, 4>>(256, each * tiles(rows, 32), Fwd<T, D, CAP, true, 4>::LDS, a, s);
+    else if (mode == ROWS_EIGHT) e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, NW>>(64 * NW, each * tiles(rows, 32 * NW), Fwd<T, D, CAP, false, NW>::LDS, a, s);
+    else e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, 4>>(256, each * tiles(rows, 128), Fwd<T, D, CAP, false, 4>::LDS, a, s);
     if (e != hipSuccess || a.splits == 1) return e;
     return launch<k_forms_join<T>>(256, (heads * rows + 3) / 4, 0, a, s);
   }
