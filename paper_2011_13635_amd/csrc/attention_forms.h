@@ -142,6 +142,22 @@ __device__ __forceinline__ f32x16_t dot_tiles(uint32_t tile, int row0, uint32_t 
     acc = mma<T>(lds_read<u32x4_t>((at ^ (32 * s)) + row0 * Tile<T, D>::ROWB), lds_read<u32x4_t>(to ^ (32 * s)), acc);
   return acc;
 }
+// How N times EACH matrix instructions (bf16), each of those fed by READS reads of LDS, are ordered: the reads of the first two go
+// out first, then each is followed by those of one further on.  Left to itself the compiler reads right before use where
+// registers are short, and a wavefront waits for LDS before every instruction (backward at 1x8192x16 heads of 128: 2.87 ms, so
+// 2.57; the forward and width 64 do not care).
+template <typename T, int N, int READS, int EACH>
+__device__ __forceinline__ void feed() {
+  if constexpr (sizeof(T) == 2) {
+    constexpr int A = N < 2 ? N : 2;
+    __builtin_amdgcn_sched_group_barrier(0x100, A * READS, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+      if (i + A < N) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+  }
+}
 // registers 8c .. 8c+7 as a B operand
 __device__ __forceinline__ bf16x8_t pack_frag(const f32x16_t& p, int c) {
   u32x4_t u;
@@ -934,6 +950,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
         f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln), dp;
         if constexpr (Q::SPARE) dp = dot_tiles<T, D>(kv.values(i), row0, lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln);
         else dp = dot_rows<T, D>(kv.values(i), row0, gf, ln);
+        feed<T, Tile<T, D>::NS, 1, 1>();
+        feed<T, Tile<T, D>::NS, Q::SPARE ? 2 : 1, 1>();
         scores<T, CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, damp);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -946,7 +964,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
           s[j] = p;
           dp[j] = ds;
         }
-        if constexpr (MEND) add_outer2<T, D>(dq, pk, kv.keys(i), row0, dp, s, ln);
+        if constexpr (MEND) {
+          add_outer2<T, D>(dq, pk, kv.keys(i), row0, dp, s, ln);
+          feed<T, D / 16, 2, 2>();
+        }
         else add_outer<T, D>(dq, kv.keys(i), row0, dp, ln);
       }
     }
@@ -980,15 +1001,15 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
 // ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
 // BLOCKS times 32 keys, over tiles of as many queries as have their rows (one for each of the G heads of the group) in RT.
 // BLOCKS wavefronts take 32 keys each; where there are more, they share the rows of a tile and add up at the end:
-//   4 of 4: 128 keys, tiles of 64 rows.  4 of 8 (bf16 at width 128): the same, two wavefronts to 32 keys; the values stay in LDS, as
-//   the accumulators and the keys fill the registers.  1 of 4 (few keys in all): 32 keys, tiles of 128 rows.
+//   4 of 4: 128 keys, tiles of 64 rows.  4 of 8 (bf16 at width 128): the same, two wavefronts to 32 keys; keys and values stay in
+//   LDS, as the accumulators fill the registers.  1 of 4 (few keys in all): 32 keys, tiles of 128 rows.
 // Few workgroups: the rows are split over a.row_splits workgroups, whose sums k_forms_kv_join adds.
 template <typename T, int D, int BLOCKS, int NW>
 struct BwdKv {
   static constexpr int PARTS = NW / BLOCKS, RT = PARTS == 4 ? 128 : 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
   static constexpr int BUFS = TILE > 32768 ? 1 : 2;
   static constexpr bool SPARE = NW == 8;
-  static constexpr int LDS = BUFS * STAGE + (SPARE ? 128 * Tile<T, D>::ROWB : 0);
+  static constexpr int LDS = BUFS * STAGE + (SPARE ? 2 * 128 * Tile<T, D>::ROWB : 0);
   struct Meta {
     float l2[RT], delta[RT], slope[RT];
     int lim[RT], id[RT], pos[RT];
@@ -1003,7 +1024,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   __shared__ TileList list;
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ __attribute__((aligned(16))) typename K::Meta meta[K::BUFS];
-  unsigned char* const Vs = lds + K::BUFS * K::STAGE;
+  unsigned char* const Ks = lds + K::BUFS * K::STAGE;
+  unsigned char* const Vs = Ks + 128 * Tile<T, D>::ROWB;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, blk = wave % BLOCKS, part = wave / BLOCKS;
   const int G = a.nh / a.nkv, QT = RT / G, used = QT * G, n_kt = (a.S + KEYS - 1) / KEYS, first = a.S - a.n;
   int bh, at;
@@ -1028,7 +1050,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   if constexpr (K::SPARE) {
     if (part == 0)
 #pragma unroll
-      for (int s = 0; s < Tile<T, D>::NS; ++s) *Tile<T, D>::at(Vs, blk * 32 + (lane & 31), 2 * s + half) = vf[s];
+      for (int s = 0; s < Tile<T, D>::NS; ++s) {
+        *Tile<T, D>::at(Ks, blk * 32 + (lane & 31), 2 * s + half) = kf[s];
+        *Tile<T, D>::at(Vs, blk * 32 + (lane & 31), 2 * s + half) = vf[s];
+      }
   }
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
@@ -1101,40 +1126,56 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
       if (!hidden) {
 #pragma unroll 1
         for (int rb = part * NR; rb < part * NR + NR; ++rb) {
-          f32x16_t s = dot_rows<T, D>(tile, 32 * rb, kf, ln), dp;
-          if constexpr (K::SPARE) dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln);
-          else dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln);
+          f32x16_t s, dp;
+          if constexpr (K::SPARE) {
+            s = dot_tiles<T, D>(tile, 32 * rb, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB, ln);
+            dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln);
+          } else {
+            s = dot_rows<T, D>(tile, 32 * rb, kf, ln);
+            dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln);
+          }
+          feed<T, Tile<T, D>::NS, K::SPARE ? 2 : 1, 1>();
+          feed<T, Tile<T, D>::NS, K::SPARE ? 2 : 1, 1>();
           f32x16_t damp;
           if constexpr (CAP) cap_scores<T, true>(sc, s, damp);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int at4 = 32 * rb + 8 * g + 4 * half;
-            const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at4), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at4);
-            float x[4];
+            if constexpr (!CAP)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = CAP ? s[4 * g + j] : sc.a * s[4 * g + j];
+              for (int j = 0; j < 4; ++j) s[4 * g + j] *= sc.a;
             if constexpr (SLOPES) {
               const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
               const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
               const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), x[j]);
+              for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), s[4 * g + j]);
             }
-            if (mask) {
+          }
+          if (mask) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const int at4 = 32 * rb + 8 * g + 4 * half;
               const int4 lm = *reinterpret_cast<const int4*>(m.lim + at4), qi = *reinterpret_cast<const int4*>(m.id + at4);
               const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[j] = key < lim[j] && (!docs || qid[j] == kid) ? x[j] : -INFINITY;
+              for (int j = 0; j < 4; ++j) s[4 * g + j] = key < lim[j] & (qid[j] == kid) ? s[4 * g + j] : -INFINITY;
             }
+          }
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int at4 = 32 * rb + 8 * g + 4 * half;
+            const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at4), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float p = __builtin_amdgcn_exp2f(x[j] - l2[j]);
+              const float p = __builtin_amdgcn_exp2f(s[4 * g + j] - l2[j]);
               s[4 * g + j] = p;
               dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
             }
           }
           add_outer<T, D>(dv, tile + TILE, 32 * rb, s, ln);
           add_outer<T, D>(dk, tile, 32 * rb, dp, ln);
+          feed<T, D / 8, 2, 1>();
         }
       }
       if (K::BUFS > 1 && i + 1 < count) commit(i + 1);
