@@ -354,8 +354,8 @@ int mslt_head_norm_workspace(int batch, int seq, int q_heads, int k_heads, int w
  * gradient.  Rows of a negative document (padding) may hold anything, NaN included: none of it is used, their outputs and
  * gradients are zeros.  All other rows must be finite, and scores within 1e30. */
 typedef struct {
-  float scale;              /* finite, > 0 */
-  float cap;                /* 0: none */
+  float scale;              /* 2^-20 to 2^20 */
+  float cap;                /* 0: none; else scale / cap 2^-24 to 2^16 */
   int causal;
   const int32_t* documents; /* DEVICE [batch, keys], or null: one document */
   const int32_t* prefix;    /* DEVICE [batch], or null; only with causal */
@@ -363,8 +363,10 @@ typedef struct {
 } mslt_attention_form;
 
 /* out = softmax(scores) v.  q, out: queries x heads; k, v: keys x kv_heads, head h reads kv head h / (heads / kv_heads).
- * 1 <= queries <= keys; heads a multiple of kv_heads; width at most 128; data, strides and width multiples of 16 bytes.
- * lse: fp32 [batch, heads, queries], natural log-sum-exp of the scores.  workspace: DEVICE scratch, 16-byte aligned, of
+ * 1 <= queries <= keys; heads a multiple of kv_heads, up to 64 times as many; width at most 128; data, strides and width
+ * multiples of 16 bytes; the rows of k and v at most 2^22 elements apart (backward: those of q and grad_out too, and the
+ * heads of a group within 2^28 elements).  keys at most 2^24, batch * heads 2^20, batch * heads * queries 2^30,
+ * batch * kv_heads * keys 2^29.  lse: fp32 [batch, heads, queries], natural log-sum-exp of the scores.  workspace: DEVICE scratch, 16-byte aligned, of
  * the bytes that mslt_attention_workspace reports for the direction. */
 int mslt_attention(void* hip_stream, int precision, int batch, int queries, int keys, int heads, int kv_heads, int width,
                    const mslt_heads* q, const mslt_heads* k, const mslt_heads* v, const mslt_attention_form* form,

@@ -402,7 +402,7 @@ def _attention_call(name, q, k, v, form, documents, prefix, slopes):
     if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
         raise _refusal(f"{name}: q {tuple(q.shape)} and k {tuple(k.shape)} must be [batch, rows, heads, width] of one batch and width")
     (B, n, h, w), (S, kv) = q.shape, k.shape[1:3]
-    f = AttentionForm(form.scale or w ** -0.5, form.cap, form.causal, _flat(name, "documents", documents, torch.int32, (B, S)),
+    f = AttentionForm(form.scale or max(w, 1) ** -0.5, form.cap, form.causal, _flat(name, "documents", documents, torch.int32, (B, S)),
                       _flat(name, "prefix", prefix, torch.int32, (B,)), _flat(name, "slopes", slopes, torch.float32, (h,)))
     return ((_precision(name, q), B, n, S, h, kv, w),
             (C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "v", v, q, k.shape))), f)

@@ -34,7 +34,6 @@ typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int LIST = 256;            // tiles listed at a time, one per thread
 constexpr float NO_MAX = -1e30f;     // running maximum before the first visible key: finite, so that differences are
-
 __device__ __forceinline__ f32x16_t zero16() {
   f32x16_t z;
 #pragma unroll
@@ -125,8 +124,7 @@ struct Lane {
 };
 // [32 tile rows from row0] x [fragment rows]: lane = fragment row, registers = tile rows
 template <typename T, int D>
-__device__ __forceinline__ f32x16_t dot_rows(uint32_t tile, int row0, const Frags<T, D>& f, const Lane<T, D>& l) {
-  f32x16_t acc = zero16();
+__device__ __forceinline__ f32x16_t dot_rows(uint32_t tile, int row0, const Frags<T, D>& f, const Lane<T, D>& l, f32x16_t acc = zero16()) {
   const uint32_t at = tile + l.rows;
 #pragma unroll
   for (int s = 0; s < Tile<T, D>::NS; ++s) acc = mma<T>(lds_read<u32x4_t>((at ^ (32 * s)) + row0 * Tile<T, D>::ROWB), f[s], acc);
@@ -134,8 +132,7 @@ __device__ __forceinline__ f32x16_t dot_rows(uint32_t tile, int row0, const Frag
 }
 // the same with the fragments read out of a second tile's rows
 template <typename T, int D>
-__device__ __forceinline__ f32x16_t dot_tiles(uint32_t tile, int row0, uint32_t other, const Lane<T, D>& l) {
-  f32x16_t acc = zero16();
+__device__ __forceinline__ f32x16_t dot_tiles(uint32_t tile, int row0, uint32_t other, const Lane<T, D>& l, f32x16_t acc = zero16()) {
   const uint32_t at = tile + l.rows, to = other + l.rows;
 #pragma unroll
   for (int s = 0; s < Tile<T, D>::NS; ++s)
@@ -220,19 +217,26 @@ __device__ __forceinline__ void add_outer2(f32x16_t (&x)[D / 32], f32x16_t (&y)[
 }
 
 // Score in base 2 from the product x of a query and a key, and what the gradient is multiplied by behind the cap.
-// tanh y = 1 - 2 / (1 + e^2y): absolute error a few 2^-24 for any y, and the score's is cap times that.  bf16, scores within six
-// tenths of the cap: y (c0 + c1 y^2 + c2 y^4 + c3 y^6) fitted to the least largest error, 5.9e-7, five multiply-adds in place of
-// two transcendental instructions (8.4 cycles each against 3) and three more.
+// tanh y = 1 - 2 / (1 + e^2y): absolute error a few 2^-24 for any y, and the score's is cap times that.  Where all of a lane's scores
+// are small against the cap, y (c0 + c1 y^2 + c2 y^4 + c3 y^6) is nearer and faster, five multiply-adds in place of two
+// transcendental instructions (8.4 cycles each against 3) and three more.  bf16: within six tenths of the cap, fitted to the least
+// largest error, 5.9e-7, relative to y 9.0e-6.  fp32: within a fifth, Taylor's, which leaves out 62/2835 y^8 < 2^-24 relative to y.  Caps above 2^16 times
+// the scale: within a twentieth, where c3 y^6 adds less than 2^-29, as the last coefficient may fall below the least fp32.
 struct Score {
   float a, c;              // no cap: s2 = a x.  cap: s2 = c tanh, exponent a x
   float p[4], reach;       // s2 = x (p0 + p1 x^2 + ...) for |x| <= reach
 };
-template <bool CAP>
+template <typename T, bool CAP>
 __device__ __forceinline__ Score make_score(float scale, float cap) {
   Score f{scale * LOG2E, 0.f, {0.f, 0.f, 0.f, 0.f}, 0.f};
   if constexpr (CAP) {
     const float y = scale / cap, u = y * y, c = cap * LOG2E;
-    f = Score{2.f * LOG2E * y, c, {c * y * 0.99999102f, c * y * u * -0.33298975f, c * y * u * u * 0.1297456f, c * y * u * u * u * -0.03961138f}, 0.6f / y};
+    f = Score{2.f * LOG2E * y, c, {0.f, 0.f, 0.f, 0.f}, (y < 0x1p-16f ? 0.05f : sizeof(T) == 2 ? 0.6f : 0.2f) / y};
+    const float k[4] = {sizeof(T) == 2 ? 0.99999102f : 1.f, sizeof(T) == 2 ? -0.33298975f : -1.f / 3.f, sizeof(T) == 2 ? 0.1297456f : 2.f / 15.f,
+                        sizeof(T) == 2 ? -0.03961138f : -17.f / 315.f};
+    float power = c * y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i, power *= u) f.p[i] = power * k[i];
   }
   return f;
 }
@@ -244,22 +248,20 @@ __device__ __forceinline__ float score2(const Score& f, float x, float& damp) {
   return f.c * t;
 }
 // the same for 16 scores at once
-template <typename T, bool DAMP>
+template <bool DAMP>
 __device__ __forceinline__ void cap_scores(const Score& f, f32x16_t& s, f32x16_t& damp) {
-  if constexpr (sizeof(T) == 2) {
-    float top = 0.f;
+  float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(s[i]));
-    if (!__any(!(top <= f.reach))) {
-      const float ic2 = 1.f / (f.c * f.c);
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(s[i]));
+  if (!__any(!(top <= f.reach))) {
+    const float ic2 = 1.f / (f.c * f.c);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float u = s[i] * s[i];
-        s[i] *= fmaf(u, fmaf(u, fmaf(u, f.p[3], f.p[2]), f.p[1]), f.p[0]);
-        if constexpr (DAMP) damp[i] = fmaf(-ic2 * s[i], s[i], 1.f);
-      }
-      return;
+    for (int i = 0; i < 16; ++i) {
+      const float u = s[i] * s[i];
+      s[i] *= fmaf(u, fmaf(u, fmaf(u, f.p[3], f.p[2]), f.p[1]), f.p[0]);
+      if constexpr (DAMP) damp[i] = fmaf(-ic2 * s[i], s[i], 1.f);
     }
+    return;
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
@@ -287,7 +289,7 @@ __device__ __forceinline__ const int2* doc_ranges(const FormArgs& a, int b, int2
 // Which tile of which kv head a workgroup takes.  Workgroups go round the eight XCDs; the tiles of one kv head are given to one
 // XCD, or to 8 / heads of them when there are fewer heads, so that its keys and values stay in few L2s.  uneven (causal): tiles
 // differ in work and come longest first; heads that do not divide so are then dealt out tile by tile, as an XCD with the
-// first tiles of a head only would finish last (1x8192, 4 kv heads: 492 us when cut into eight runs, TODO us so).
+// first tiles of a head only would finish last (1x8192, 4 kv heads: 492 us when each XCD has a run of tiles, 381 us in turn).
 __device__ __forceinline__ void tile_order(int id, int heads, int tiles, bool uneven, int& head, int& tile) {
   const int x = id & 7, i = id >> 3;
   if (heads % 8 == 0) {
@@ -356,7 +358,7 @@ __device__ __forceinline__ void load_frags(Frags<T, D>& f, const T* row, int hal
 // lane fetches is free, which is where the swizzle lives.  A lane whose piece is none of the operand's (a row past the end, a
 // row of padding, elements past the width) fetches beyond the buffer's end, which writes zeros.
 // The load is written out: behind the builtin the compiler lets every transposed read wait for all loads on their way, as it
-// cannot tell the tiles apart (1x8192, 16 heads of 128: 367 us, TODO us without).  It returns nothing to a register; wait_loads()
+// cannot tell the tiles apart (1x8192, 16 heads of 128, backward: queries 801 us, 689 written out; keys 1090, 924).  It returns nothing to a register; wait_loads()
 // and a barrier stand between it and the reads.
 constexpr uint32_t NOWHERE = 0x80000000u;
 struct Source {
@@ -540,9 +542,9 @@ __device__ __forceinline__ void positions_range(const int2* r, int p0, int p1, i
 // score_factor() is the score in base 2; without cap and distance that leaves the factor to the exponential's own multiply-add.
 template <bool CAP, bool SLOPES>
 __device__ __forceinline__ float score_factor(const Score& f) { return CAP || SLOPES ? 1.f : f.a; }
-template <typename T, bool CAP, bool SLOPES, bool DAMP>
+template <bool CAP, bool SLOPES, bool DAMP>
 __device__ __forceinline__ void open_scores(const Score& f, const RowOf& r, int k0, int half, f32x16_t& s, f32x16_t& damp) {
-  if constexpr (CAP) cap_scores<T, DAMP>(f, s, damp);
+  if constexpr (CAP) cap_scores<DAMP>(f, s, damp);
   if constexpr (SLOPES) {
     const float far = (float)(r.pos - k0 - 4 * half), c = CAP ? 1.f : f.a;
 #pragma unroll
@@ -566,10 +568,10 @@ __device__ __forceinline__ void hide(const FormArgs& a, const RowOf& r, const in
     }
   }
 }
-template <typename T, bool CAP, bool SLOPES, bool DAMP>
+template <bool CAP, bool SLOPES, bool DAMP>
 __device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int limit, int half, bool mask,
                                        f32x16_t& s, f32x16_t& damp) {
-  open_scores<T, CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
+  open_scores<CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
   if (mask) hide(a, r, ids, k0, limit, half, s);
 }
 
@@ -675,7 +677,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
   const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, F::ROWS, prefix, wave, lane);
   Frags<T, D> qf;
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
-  const Score sc = make_score<CAP>(a.scale, a.cap);
+  const Score sc = make_score<T, CAP>(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename F::Keys kv;
@@ -731,7 +733,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
       for (int kb = 0; kb < NK; ++kb) {
         const int row0 = 32 * (kb0 + kb);
         f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln);
-        scores<T, CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, unused);
+        scores<CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, unused);
         refer(factor * row_top(s));
         powers(s);
         add_outer<T, D>(o, kv.values(i), row0, s, ln);
@@ -765,7 +767,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
     }
     const RowOf rr = row_of(a, R, b, hk, prefix);
     if (!rr.in) return;
-    const bool some = rr.live && l > 0.f;
+    const bool some = rr.live && l != 0.f;      // (a NaN stays one)
     const size_t prow = ((size_t)split * a.B * a.nkv + (size_t)b * a.nkv + hk) * rows + R;
     const float inv = a.splits > 1 ? 1.f : some ? 1.f / l : 0.f;
     T* const out = head_out<T>(a.o, b, rr.head) + (long long)rr.qi * a.o.sr;
@@ -783,7 +785,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
     }
   } else {
     if (!r.in) return;
-    const bool some = r.live && l_run > 0.f;
+    const bool some = r.live && l_run != 0.f;      // (a NaN stays one)
     if (a.splits > 1) {
       const size_t prow = ((size_t)split * a.B * a.nkv + (size_t)b * a.nkv + hk) * rows + r.R;
       store_row<float, D>(a.part + prow * a.w, o, half, a.w, 1.f, true);
@@ -795,27 +797,47 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
   }
 }
 
-// Results of the workgroups that shared a row's keys: put onto the largest maximum, added in their order.  One wavefront a row.
+// Results of the workgroups that shared a row's keys: put onto the largest maximum, added in their order.  One wavefront a row;
+// its halves take every second workgroup, and lane i of the first ones workgroup i's maximum and sum.
 template <typename T>
 __global__ void __launch_bounds__(256) k_forms_join(FormArgs a) {
-  const int lane = threadIdx.x & 63, G = a.nh / a.nkv, rows = a.n * G;
-  const size_t total = (size_t)a.B * a.nkv * rows, row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ float e_s[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, G = a.nh / a.nkv, rows = a.n * G;
+  const size_t total = (size_t)a.B * a.nkv * rows, row = (size_t)blockIdx.x * 4 + wave;
   if (row >= total) return;
+  const float2 none = make_float2(NO_MAX, 0.f);
   float m = NO_MAX, l = 0.f;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[s * total + row].x);
   f32x4_t x = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int d = 4 * lane;
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = a.part_ml[s * total + row];
-    const float e = __builtin_amdgcn_exp2f(ml.x - m);
-    l += e * ml.y;
-    if (d < a.w && ml.y > 0.f) x += *reinterpret_cast<const f32x4_t*>(a.part + (s * total + row) * a.w + d) * e;
+  const int d = 4 * (lane & 31);
+  for (int base = 0; base < a.splits; base += 64) {
+    const int n = min(64, a.splits - base);
+    const float2 ml = lane < n ? a.part_ml[(size_t)(base + lane) * total + row] : none;
+    float top = ml.x;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    const float m_new = fmaxf(m, top), old = __builtin_amdgcn_exp2f(m - m_new), e = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - m_new) : 0.f;
+    l = l * old + wave_sum(e * ml.y);
+    x *= old;
+    m = m_new;
+    e_s[wave][lane] = e;
+    __builtin_amdgcn_wave_barrier();
+    if (d < a.w)
+#pragma unroll 8
+      for (int s = half; s < n; s += 2) {
+        const float f = e_s[wave][s];
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.part + ((size_t)(base + s) * total + row) * a.w + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = f != 0.f ? fmaf(v[j], f, x[j]) : x[j];
+      }
+    __builtin_amdgcn_wave_barrier();
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] += __shfl_xor(x[j], 32, 64);
   const int R = (int)(row % rows), hk = (int)(row / rows) % a.nkv, b = (int)(row / ((size_t)rows * a.nkv));
   const int head = hk * G + R % G, qi = R / G;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  if (d < a.w) store4(head_out<T>(a.o, b, head) + (long long)qi * a.o.sr + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-  if (lane == 0) a.lse[((size_t)b * a.nh + head) * a.n + qi] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  if (half == 0 && d < a.w) store4(head_out<T>(a.o, b, head) + (long long)qi * a.o.sr + d, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+  if (lane == 0) a.lse[((size_t)b * a.nh + head) * a.n + qi] = l != 0.f ? (m + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
 }
 
 // Sums of PARTS wavefronts that worked on the same rows (or keys), of which a workgroup has BLOCKS: the others' through LDS onto
@@ -897,7 +919,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const int R0 = rt * Q::ROWS, Rw = __builtin_amdgcn_readfirstlane(R0 + row_blk * 32);
   const RowOf r = row_of(a, Rw + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, Q::ROWS, prefix, wave, lane);
-  const Score sc = make_score<CAP>(a.scale, a.cap);
+  const Score sc = make_score<T, CAP>(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename Q::Keys kv;
@@ -952,7 +974,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
         else dp = dot_rows<T, D>(kv.values(i), row0, gf, ln);
         feed<T, Tile<T, D>::NS, 1, 1>();
         feed<T, Tile<T, D>::NS, Q::SPARE ? 2 : 1, 1>();
-        scores<T, CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, damp);
+        scores<CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, damp);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
@@ -998,6 +1020,18 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
 }
 
+// the 16 of 32 rows' values that this half-wave's registers stand for
+__device__ __forceinline__ f32x16_t rows_of(const float* x, int half) {
+  f32x16_t r;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(x + 8 * g + 4 * half);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[4 * g + j] = v[j];
+  }
+  return r;
+}
+
 // ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
 // BLOCKS times 32 keys, over tiles of as many queries as have their rows (one for each of the G heads of the group) in RT.
 // BLOCKS wavefronts take 32 keys each; where there are more, they share the rows of a tile and add up at the end:
@@ -1011,7 +1045,7 @@ struct BwdKv {
   static constexpr bool SPARE = NW == 8;
   static constexpr int LDS = BUFS * STAGE + (SPARE ? 2 * 128 * Tile<T, D>::ROWB : 0);
   struct Meta {
-    float l2[RT], delta[RT], slope[RT];
+    float l2[RT], delta[RT], slope[RT];        // -log-sum-exp in base 2 (PLAIN: over the score's factor), -delta
     int lim[RT], id[RT], pos[RT];
   };
   static_assert(BUFS * STAGE >= (PARTS - 1) * BLOCKS * 32 * D * 4, "the sums' room");
@@ -1019,7 +1053,8 @@ struct BwdKv {
 template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW>
 __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8) ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
   using K = BwdKv<T, D, BLOCKS, NW>;
-  constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;      // NR: blocks of 32 rows of a tile that a wavefront takes
+  constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;
+  constexpr bool PLAIN = !CAP && !SLOPES;  // NR: blocks of 32 rows of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
@@ -1039,7 +1074,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const int kid = docs ? (in ? docs[key] : -1) : 0;
   const bool live = in && kid >= 0;
   const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
-  const Score sc = make_score<CAP>(a.scale, a.cap);
+  const Score sc = make_score<T, CAP>(a.scale, a.cap);
   const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
   int klo, khi;
   positions_range(ranges, kt * KEYS, min(a.S, kt * KEYS + KEYS) - 1, klo, khi);
@@ -1085,8 +1120,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   auto commit = [&](int i) {
     if (tid >= RT) return;
     typename K::Meta& m = meta[i & (K::BUFS - 1)];
-    m.l2[tid] = ml2 == -INFINITY ? INFINITY : ml2 * LOG2E;     // rows that see nothing: probabilities zero
-    m.delta[tid] = mdelta;
+    m.l2[tid] = ml2 == -INFINITY ? -INFINITY : -ml2 * (PLAIN ? LOG2E / sc.a : LOG2E);     // rows that see nothing: probabilities zero
+    m.delta[tid] = -mdelta;
     m.slope[tid] = mr.slope2;
     m.lim[tid] = mr.lim;
     m.id[tid] = mr.id;
@@ -1126,30 +1161,28 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
       if (!hidden) {
 #pragma unroll 1
         for (int rb = part * NR; rb < part * NR + NR; ++rb) {
-          f32x16_t s, dp;
+          // without cap and slopes the products start from what is taken off them, the row's log-sum-exp and delta
+          f32x16_t s = PLAIN ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
           if constexpr (K::SPARE) {
-            s = dot_tiles<T, D>(tile, 32 * rb, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB, ln);
-            dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln);
+            s = dot_tiles<T, D>(tile, 32 * rb, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB, ln, s);
+            dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln, dp);
           } else {
-            s = dot_rows<T, D>(tile, 32 * rb, kf, ln);
-            dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln);
+            s = dot_rows<T, D>(tile, 32 * rb, kf, ln, s);
+            dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln, dp);
           }
           feed<T, Tile<T, D>::NS, K::SPARE ? 2 : 1, 1>();
           feed<T, Tile<T, D>::NS, K::SPARE ? 2 : 1, 1>();
           f32x16_t damp;
-          if constexpr (CAP) cap_scores<T, true>(sc, s, damp);
+          if constexpr (CAP) cap_scores<true>(sc, s, damp);
+          if constexpr (SLOPES) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int at4 = 32 * rb + 8 * g + 4 * half;
-            if constexpr (!CAP)
-#pragma unroll
-              for (int j = 0; j < 4; ++j) s[4 * g + j] *= sc.a;
-            if constexpr (SLOPES) {
+            for (int g = 0; g < 4; ++g) {
+              const int at4 = 32 * rb + 8 * g + 4 * half;
               const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
               const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
               const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
 #pragma unroll
-              for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), s[4 * g + j]);
+              for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), (CAP ? 1.f : sc.a) * s[4 * g + j]);
             }
           }
           if (mask) {
@@ -1164,13 +1197,16 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
           }
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const int at4 = 32 * rb + 8 * g + 4 * half;
-            const f32x4_t l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + at4), dl = *reinterpret_cast<const f32x4_t*>(m.delta + at4);
+            f32x4_t l2 = f32x4_t{0.f, 0.f, 0.f, 0.f}, dl = l2;
+            if constexpr (!PLAIN) {
+              l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
+              dl = *reinterpret_cast<const f32x4_t*>(m.delta + 32 * rb + 8 * g + 4 * half);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float p = __builtin_amdgcn_exp2f(s[4 * g + j] - l2[j]);
+              const float p = __builtin_amdgcn_exp2f(PLAIN ? sc.a * s[4 * g + j] : s[4 * g + j] + l2[j]);
               s[4 * g + j] = p;
-              dp[4 * g + j] = p * (dp[4 * g + j] - dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
+              dp[4 * g + j] = p * (PLAIN ? dp[4 * g + j] : dp[4 * g + j] + dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
             }
           }
           add_outer<T, D>(dv, tile + TILE, 32 * rb, s, ln);
@@ -1233,7 +1269,8 @@ inline hipError_t launch(int threads, size_t blocks, int lds, const FormArgs& a,
 // How the rows (and, backward, the keys) are dealt out: four wavefronts to 32 rows where there are few, 32 rows to each of eight
 // (width 128 in bf16) where there are many; see attention_forms_bf16.hip.
 enum RowMode { ROWS_FEW, ROWS_FOUR, ROWS_EIGHT };
-RowMode row_mode(bool wide, size_t heads, int rows);
+RowMode row_mode(bool wide, int w, size_t heads, int rows);
+bool few_keys(int w, size_t heads, int keys);
 
 template <typename T, int D, bool CAP, bool SLOPES>
 struct Launch {
@@ -1243,7 +1280,7 @@ struct Launch {
   static hipError_t fwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv, each = heads * a.splits;
-    const RowMode mode = row_mode(WIDE, heads, rows);
+    const RowMode mode = row_mode(WIDE, D, heads, rows);
     hipError_t e;
     if (mode == ROWS_FEW) e = launch<k_forms_fwd<T, D, CAP, SLOPES, true, 4>>(256, each * tiles(rows, 32), Fwd<T, D, CAP, true, 4>::LDS, a, s);
     else if (mode == ROWS_EIGHT) e = launch<k_forms_fwd<T, D, CAP, SLOPES, false, NW>>(64 * NW, each * tiles(rows, 32 * NW), Fwd<T, D, CAP, false, NW>::LDS, a, s);
@@ -1254,13 +1291,13 @@ struct Launch {
   static hipError_t bwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv;
-    const RowMode mode = row_mode(WIDE, heads, rows);
+    const RowMode mode = row_mode(WIDE, D, heads, rows);
     hipError_t e;
     if (mode == ROWS_FEW) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, true, 4>>(256, heads * tiles(rows, 32), BwdQ<T, D, true, 4>::LDS, a, s);
     else if (mode == ROWS_EIGHT) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, 32 * NW), BwdQ<T, D, false, NW>::LDS, a, s);
     else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
     if (e != hipSuccess) return e;
-    if (row_mode(false, heads, a.S) == ROWS_FEW)
+    if (few_keys(D, heads, a.S))
       e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 1, 4>>(256, heads * tiles(a.S, 32) * a.row_splits, BwdKv<T, D, 1, 4>::LDS, a, s);
     else e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 4, NW>>(64 * NW, heads * tiles(a.S, 128) * a.row_splits, BwdKv<T, D, 4, NW>::LDS, a, s);
     if (e != hipSuccess || a.row_splits == 1) return e;

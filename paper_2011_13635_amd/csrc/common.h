@@ -270,9 +270,9 @@ struct FormArgs {
 };
 constexpr int FORM_OWN_RANGES = 64;      // blocks of 64 positions whose documents a workgroup looks at itself
 // Parts the forward splits the keys into.
-int form_splits(int B, int n, int S, int nh, int nkv);
+int form_splits(int B, int n, int S, int nh, int nkv, int w);
 // Parts the key side of the backward splits the rows into.
-int form_row_splits(int B, int n, int S, int nh, int nkv);
+int form_row_splits(int B, int n, int S, int nh, int nkv, int w);
 hipError_t form_ranges(const FormArgs& a, hipStream_t s);
 hipError_t form_fwd_bf16(const FormArgs& a, hipStream_t s);
 hipError_t form_fwd_f32(const FormArgs& a, hipStream_t s);

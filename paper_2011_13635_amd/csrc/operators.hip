@@ -83,9 +83,8 @@ static int rotary_form(const char* who, const mslt_rotary_form* f, int width, Ro
   }
   return MSLT_OK;
 }
-static int run_rotary(const char* who, void* stream, int precision, const RotaryArgs& a, bool backward) {
+static int run_rotary(void* stream, int precision, const RotaryArgs& a, bool backward) {
   HIP_TRY(rotary_run(precision, a, backward, reinterpret_cast<hipStream_t>(stream)));
-  (void)who;
   return MSLT_OK;
 }
 
@@ -108,7 +107,7 @@ extern "C" int mslt_rotary(void* hip_stream, int precision, int batch, int seq, 
   a.q = heads_of(q), a.k = heads_of(k), a.oq = heads_of(q_out), a.ok = heads_of(k ? k_out : nullptr);
   a.positions = positions;
   a.B = batch, a.S = seq, a.hq = q_heads, a.hk = k_heads, a.w = width, a.inverse = inverse != 0;
-  return run_rotary(who, hip_stream, precision, a, false);
+  return run_rotary(hip_stream, precision, a, false);
 }
 
 static int norm_args(const char* who, int precision, int batch, int seq, int q_heads, int k_heads, int width, const mslt_heads* q,
@@ -140,7 +139,7 @@ extern "C" int mslt_head_norm_rotary(void* hip_stream, int precision, int batch,
   HEADS_OK(q_out, seq, q_heads, false, true);
   HEADS_OK(k_out, seq, k_heads, false, true);
   a.oq = heads_of(q_out), a.ok = heads_of(k_out);
-  return run_rotary(who, hip_stream, precision, a, false);
+  return run_rotary(hip_stream, precision, a, false);
 }
 
 extern "C" int mslt_head_norm_workspace(int batch, int seq, int q_heads, int k_heads, int width, size_t* bytes) {
@@ -172,7 +171,7 @@ extern "C" int mslt_head_norm_rotary_backward(void* hip_stream, int precision, i
     return fail(MSLT_ERR_ARG, "%s: needs a workspace of %zu bytes, 16-byte aligned", who, need);
   a.gq = heads_of(grad_q), a.gk = heads_of(grad_k), a.oq = heads_of(dq), a.ok = heads_of(dk);
   a.dgain_q = dgain_q, a.dgain_k = dgain_k, a.partial = static_cast<float*>(workspace);
-  return run_rotary(who, hip_stream, precision, a, true);
+  return run_rotary(hip_stream, precision, a, true);
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------
@@ -182,10 +181,10 @@ static int attention_sizes(const char* who, int precision, int batch, int querie
     return fail(MSLT_ERR_ARG, "%s: needs 1 <= queries <= keys and heads a multiple of kv_heads", who);
   if (heads / kv_heads > 64) return fail(MSLT_ERR_ARG, "%s: more than 64 heads to a kv head", who);
   if (width > 128 || width % (precision ? 8 : 4)) return fail(MSLT_ERR_ARG, "%s: width must be a multiple of 16 bytes, at most 128", who);
-  // positions as fp32 and tiles as a grid
-  if (keys > (1 << 24) || (long long)batch * heads > (1 << 20) || (long long)batch * heads * keys > (1ll << 34) ||
-      (long long)heads * queries > (1ll << 30))
-    return fail(MSLT_ERR_ARG, "%s: more than 2^24 keys, 2^20 heads, 2^34 keys of all heads or 2^30 rows of a sequence", who);
+  // positions as fp32, and a grid of fewer than 2^32 threads: two to a row of a head, four to a key of a kv head
+  const long long all = (long long)batch * heads;
+  if (keys > (1 << 24) || all > (1 << 20) || all * queries > (1ll << 30) || all / heads * kv_heads * keys > (1ll << 29))
+    return fail(MSLT_ERR_ARG, "%s: more than 2^24 keys, 2^20 heads, 2^30 queries of all heads or 2^29 keys of all kv heads", who);
   return MSLT_OK;
 }
 namespace {
@@ -197,14 +196,14 @@ Workspace attention_layout(int precision, int batch, int queries, int keys, int 
   Workspace w{};
   const size_t rows = (size_t)batch * heads * queries;
   size_t at = up((size_t)batch * ((keys + 63) / 64) * sizeof(int2));
-  *splits = backward ? 1 : form_splits(batch, queries, keys, heads, kv_heads);
+  *splits = backward ? 1 : form_splits(batch, queries, keys, heads, kv_heads, width);
   if (*splits > 1) {
     w.part = at;
     at += up(rows * *splits * width * sizeof(float));
     w.part_ml = at;
     at += up(rows * *splits * sizeof(float2));
   }
-  *row_splits = backward ? form_row_splits(batch, queries, keys, heads, kv_heads) : 1;
+  *row_splits = backward ? form_row_splits(batch, queries, keys, heads, kv_heads, width) : 1;
   if (*row_splits > 1) {
     w.part = at;
     at += up((size_t)2 * *row_splits * batch * kv_heads * keys * width * sizeof(float));
@@ -239,8 +238,10 @@ static int attention_args(const char* who, int precision, int batch, int queries
   if (keys > 1 && (k->row_stride > (1 << 22) || v->row_stride > (1 << 22)))
     return fail(MSLT_ERR_ARG, "%s: a row stride of k or v above 2^22 elements", who);
   if (!f) return fail(MSLT_ERR_ARG, "%s: form is null", who);
-  if (!(f->scale > 0.f) || !std::isfinite(f->scale)) return fail(MSLT_ERR_ARG, "%s: scale must be above 0", who);
-  if (!(f->cap >= 0.f) || !std::isfinite(f->cap)) return fail(MSLT_ERR_ARG, "%s: cap must be 0 or above", who);
+  // (the kernels divide by the scale, and take (scale / cap)^7 cap)
+  if (!(f->scale >= 0x1p-20f && f->scale <= 0x1p20f)) return fail(MSLT_ERR_ARG, "%s: scale must be 2^-20 to 2^20", who);
+  if (!(f->cap == 0.f || (f->cap >= f->scale * 0x1p-16f && f->cap <= f->scale * 0x1p24f)))
+    return fail(MSLT_ERR_ARG, "%s: cap must be 0, or scale / cap 2^-24 to 2^16", who);
   if (f->prefix && !f->causal) return fail(MSLT_ERR_ARG, "%s: a prefix needs causal", who);
   const Workspace w = attention_layout(precision, batch, queries, keys, heads, kv_heads, width, backward, &a.splits, &a.row_splits);
   if (!workspace || workspace_bytes < w.total || reinterpret_cast<uintptr_t>(workspace) % 16)

@@ -129,6 +129,44 @@ def test_large_scores_stay_finite(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(2, 70, 70, 4, 2, 64), (1, 1, 2000, 4, 2, 128), (64, 128, 128, 8, 8, 64), (64, 260, 260, 4, 4, 128)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_what_is_not_a_number_stays_so(shape, dtype):
+    import torch
+    B, n, S, h, kv, w = shape
+    dt = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn(s, generator=g, device="cuda").to(dt) for s in ((B, n, h, w), (B, S, kv, w), (B, S, kv, w)))
+    q[0, n // 2, 1, 3] = float("nan")
+    for cap in (0.0, 30.0):
+        form = binding.attention_form(cap=cap)
+        f = binding.mslt_attention(q, k, v, form)
+        d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], torch.ones_like(q), form)
+        bad = torch.zeros((B, n, h), dtype=torch.bool, device="cuda")
+        bad[0, n // 2, 1] = True
+        assert torch.equal(bad, torch.isnan(f["lse"]).transpose(1, 2))
+        for x in (f["out"], d["dq"]):
+            assert torch.equal(bad[..., None].expand_as(x), torch.isnan(x))
+        for x in (d["dk"], d["dv"]):      # its kv head's
+            assert torch.isnan(x[0, :, 1 // (h // kv)]).all() and not torch.isnan(x[1:]).any()
+
+
+def test_a_cap_far_above_the_scores():
+    # Scores of some tens under a cap of 10^5: what the cap takes off is below 10^-5 of them, and no more may get lost than without a
+    # cap.  The bounds are those without (16 roundings of a score's terms): the polynomial adds five and what it leaves out, one.
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v, go = (torch.randn((2, 90, 2, 64), generator=g, device="cuda").mul(s) for s in (3, 3, 1, 1))
+    form = binding.attention_form(cap=1e5, scale=0.25)
+    f = binding.mslt_attention(q, k, v, form)
+    d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form)
+    want, _ = R.attention(q, k, v, cap=1e5, scale=0.25, grad=go)
+    bounds, _ = R.attention(q, k, v, scale=0.25, grad=go)
+    for name in want:
+        R.check({**f, **d}[name], (want[name][0], *bounds[name][1:]), False, name)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_layouts(dtype):
     """Heads before tokens, rows apart, a batch that is broadcast, results into parts of a packed tensor: the same values."""
     import torch

@@ -75,6 +75,37 @@ def test_attention_operands(operand, backward):
     _refused(_attention(backward=backward, room=8), "workspace")
 
 
+@pytest.mark.parametrize("sizes,text", [
+    ({"heads": 65, "kv_heads": 1}, "64 heads"), ({"batch": 1 << 18, "queries": 1 << 12, "keys": 1 << 12, "kv_heads": 1}, "2^30 queries"),
+    ({"batch": 1 << 15, "queries": 1, "keys": 1 << 14}, "2^29 keys")])
+@pytest.mark.parametrize("backward", [False, True])
+def test_attention_limits(sizes, text, backward):
+    s = {**ATT, **sizes}
+    _refused(_attention(sizes, backward=backward), text)
+    n = C.c_size_t()
+    _refused(b.load_library().mslt_attention_workspace(*s.values(), int(backward), C.byref(n)), text)
+    # one step inside them
+    inside = {"heads": 64} if s["heads"] == 65 else {"batch": s["batch"] // 2}
+    assert b.load_library().mslt_attention_workspace(*{**s, **inside}.values(), int(backward), C.byref(n)) == 0
+
+
+@pytest.mark.parametrize("form", [{"scale": 2.0 ** -21}, {"scale": 2.0 ** 21}, {"scale": 1.0, "cap": 2.0 ** -17}, {"scale": 1.0, "cap": 2.0 ** 25}])
+def test_attention_factors_out_of_range(form):
+    _refused(_attention(form=form), "2^")
+    _refused(_attention(form=form, backward=True), "2^")
+
+
+def test_attention_strides_out_of_reach():
+    far = (1 << 22) + 8
+    for name in ("k", "v"):
+        for backward in (False, True):
+            _refused(_attention(backward=backward, **{name: _heads(row_stride=far)}), "2^22")
+    grouped = {"heads": 4, "kv_heads": 2}
+    for name in ("q", "grad_out"):
+        _refused(_attention(backward=True, **{name: _heads(row_stride=far)}), "2^22")
+        _refused(_attention(grouped, backward=True, **{name: _heads(head_stride=(1 << 27) + 8)}), "2^28")
+
+
 def test_attention_workspace_counts_split_keys_and_rows():
     n, f, g = C.c_size_t(), C.c_size_t(), C.c_size_t()
     lib = b.load_library()
@@ -165,5 +196,7 @@ def test_binding_refuses():
     for t in (torch.zeros(4), torch.zeros(3, dtype=torch.int32), torch.zeros(8, dtype=torch.int32)[::2]):
         with pytest.raises(b.MsltError):
             b._flat("f", "x", t, torch.int32, (4,))
+    form, none = b.attention_form(), x[..., :0]
+    assert b._attention_call("f", none, none, none, form, None, None, None)[0][-1] == 0        # (the library refuses the width)
     with pytest.raises(b.MsltError):
         b._rotary_sizes("f", x, torch.zeros(1, 3, 2, 64))
