@@ -355,7 +355,7 @@ int mslt_head_norm_workspace(int batch, int seq, int q_heads, int k_heads, int w
  * gradients are zeros.  All other rows must be finite, and scores within 1e30. */
 typedef struct {
   float scale;              /* 2^-20 to 2^20 */
-  float cap;                /* 0: none; else scale / cap 2^-24 to 2^16 */
+  float cap;                /* 0: none; else scale / cap 2^-24 to 2^12 */
   int causal;
   const int32_t* documents; /* DEVICE [batch, keys], or null: one document */
   const int32_t* prefix;    /* DEVICE [batch], or null; only with causal */

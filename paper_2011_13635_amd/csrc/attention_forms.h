@@ -218,25 +218,25 @@ __device__ __forceinline__ void add_outer2(f32x16_t (&x)[D / 32], f32x16_t (&y)[
 
 // Score in base 2 from the product x of a query and a key, and what the gradient is multiplied by behind the cap.
 // tanh y = 1 - 2 / (1 + e^2y): absolute error a few 2^-24 for any y, and the score's is cap times that.  Where all of a lane's scores
-// are small against the cap, y (c0 + c1 y^2 + c2 y^4 + c3 y^6) is nearer and faster, five multiply-adds in place of two
-// transcendental instructions (8.4 cycles each against 3) and three more.  bf16: within six tenths of the cap, fitted to the least
-// largest error, 5.9e-7, relative to y 9.0e-6.  fp32: within a fifth, Taylor's, which leaves out 62/2835 y^8 < 2^-24 relative to y.  Caps above 2^16 times
-// the scale: within a twentieth, where c3 y^6 adds less than 2^-29, as the last coefficient may fall below the least fp32.
+// lie within six tenths of the cap, y (c0 + c1 y^2 + .. + c4 y^8) is nearer and faster, six multiply-adds in place of two
+// transcendental instructions (8.4 cycles each against 3) and three more; fitted to the least largest error relative to y, 7.4e-8.
+// Caps so far above the scale that c4's factor falls below the least fp32: within a twentieth, where c3 y^6 adds less than 2^-29.
 struct Score {
   float a, c;              // no cap: s2 = a x.  cap: s2 = c tanh, exponent a x
-  float p[4], reach;       // s2 = x (p0 + p1 x^2 + ...) for |x| <= reach
+  float p[5], reach;       // s2 = x (p0 + p1 x^2 + ...) for |x| <= reach
 };
-template <typename T, bool CAP>
+template <bool CAP>
 __device__ __forceinline__ Score make_score(float scale, float cap) {
-  Score f{scale * LOG2E, 0.f, {0.f, 0.f, 0.f, 0.f}, 0.f};
+  Score f{scale * LOG2E, 0.f, {0.f, 0.f, 0.f, 0.f, 0.f}, 0.f};
   if constexpr (CAP) {
-    const float y = scale / cap, u = y * y, c = cap * LOG2E;
-    f = Score{2.f * LOG2E * y, c, {0.f, 0.f, 0.f, 0.f}, (y < 0x1p-16f ? 0.05f : sizeof(T) == 2 ? 0.6f : 0.2f) / y};
-    const float k[4] = {sizeof(T) == 2 ? 0.99999102f : 1.f, sizeof(T) == 2 ? -0.33298975f : -1.f / 3.f, sizeof(T) == 2 ? 0.1297456f : 2.f / 15.f,
-                        sizeof(T) == 2 ? -0.03961138f : -17.f / 315.f};
-    float power = c * y;
+    constexpr float fit[5] = {0.99999993f, -0.3333231f, 0.13310174f, -0.05210148f, 0.01547543f};
+    const float y = scale / cap;
+    f.a = 2.f * LOG2E * y;
+    f.c = cap * LOG2E;
+    float power = f.c * y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i, power *= u) f.p[i] = power * k[i];
+    for (int i = 0; i < 5; ++i, power *= y * y) f.p[i] = power * fit[i];
+    f.reach = (f.p[4] < 0x1p-126f ? 0.05f : 0.6f) / y;
   }
   return f;
 }
@@ -258,7 +258,7 @@ __device__ __forceinline__ void cap_scores(const Score& f, f32x16_t& s, f32x16_t
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float u = s[i] * s[i];
-      s[i] *= fmaf(u, fmaf(u, fmaf(u, f.p[3], f.p[2]), f.p[1]), f.p[0]);
+      s[i] *= fmaf(u, fmaf(u, fmaf(u, fmaf(u, f.p[4], f.p[3]), f.p[2]), f.p[1]), f.p[0]);
       if constexpr (DAMP) damp[i] = fmaf(-ic2 * s[i], s[i], 1.f);
     }
     return;
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
   const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, F::ROWS, prefix, wave, lane);
   Frags<T, D> qf;
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
-  const Score sc = make_score<T, CAP>(a.scale, a.cap);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename F::Keys kv;
@@ -919,7 +919,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const int R0 = rt * Q::ROWS, Rw = __builtin_amdgcn_readfirstlane(R0 + row_blk * 32);
   const RowOf r = row_of(a, Rw + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, Q::ROWS, prefix, wave, lane);
-  const Score sc = make_score<T, CAP>(a.scale, a.cap);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
   const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename Q::Keys kv;
@@ -1074,7 +1074,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const int kid = docs ? (in ? docs[key] : -1) : 0;
   const bool live = in && kid >= 0;
   const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
-  const Score sc = make_score<T, CAP>(a.scale, a.cap);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
   const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
   int klo, khi;
   positions_range(ranges, kt * KEYS, min(a.S, kt * KEYS + KEYS) - 1, klo, khi);

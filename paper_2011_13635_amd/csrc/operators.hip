@@ -238,10 +238,10 @@ static int attention_args(const char* who, int precision, int batch, int queries
   if (keys > 1 && (k->row_stride > (1 << 22) || v->row_stride > (1 << 22)))
     return fail(MSLT_ERR_ARG, "%s: a row stride of k or v above 2^22 elements", who);
   if (!f) return fail(MSLT_ERR_ARG, "%s: form is null", who);
-  // (the kernels divide by the scale, and take (scale / cap)^7 cap)
+  // (the kernels divide by the scale, and take (scale / cap)^9 cap)
   if (!(f->scale >= 0x1p-20f && f->scale <= 0x1p20f)) return fail(MSLT_ERR_ARG, "%s: scale must be 2^-20 to 2^20", who);
-  if (!(f->cap == 0.f || (f->cap >= f->scale * 0x1p-16f && f->cap <= f->scale * 0x1p24f)))
-    return fail(MSLT_ERR_ARG, "%s: cap must be 0, or scale / cap 2^-24 to 2^16", who);
+  if (!(f->cap == 0.f || (f->cap >= f->scale * 0x1p-12f && f->cap <= f->scale * 0x1p24f)))
+    return fail(MSLT_ERR_ARG, "%s: cap must be 0, or scale / cap 2^-24 to 2^12", who);
   if (f->prefix && !f->causal) return fail(MSLT_ERR_ARG, "%s: a prefix needs causal", who);
   const Workspace w = attention_layout(precision, batch, queries, keys, heads, kv_heads, width, backward, &a.splits, &a.row_splits);
   if (!workspace || workspace_bytes < w.total || reinterpret_cast<uintptr_t>(workspace) % 16)
