@@ -897,6 +897,36 @@ struct BwdQ {
   static constexpr int LDS = Keys::LDS + (SPARE ? ROWS * Tile<T, D>::ROWB : 0);
   static_assert(!FEW || Keys::LDS >= 3 * 32 * D * 4 + 3 * 256, "the join's room");
 };
+// A wavefront's 32 rows and 32 keys from k0 on, row0 in the tiles of keys and values: dQ, the sums of p damp k and rest grow.
+template <typename T, int D, bool CAP, bool SLOPES, bool MEND, bool SPARE>
+__device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, const RowOf& r, uint32_t keys, uint32_t values, int row0, const int* ids,
+                                            int k0, int limit, bool mask, const Frags<T, D>& qf, const Frags<T, D>& gf, uint32_t grad, const Lane<T, D>& ln,
+                                            int half, float l2, float delta, f32x16_t (&dq)[D / 32], f32x16_t (&pk)[MEND ? D / 32 : 1], float& rest) {
+  const float factor = score_factor<CAP, SLOPES>(sc);
+  f32x16_t s = dot_rows<T, D>(keys, row0, qf, ln), dp, damp;
+  if constexpr (SPARE) dp = dot_tiles<T, D>(values, row0, grad, ln);
+  else dp = dot_rows<T, D>(values, row0, gf, ln);
+  feed<T, Tile<T, D>::NS, 1, 1>();
+  feed<T, Tile<T, D>::NS, SPARE ? 2 : 1, 1>();
+  scores<CAP, SLOPES, true>(a, sc, r, ids, k0, limit, half, mask, s, damp);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
+    if constexpr (MEND) rest += ds;
+    if constexpr (CAP) {
+      ds *= damp[j];
+      p *= damp[j];
+    }
+    s[j] = p;
+    dp[j] = ds;
+  }
+  if constexpr (MEND) {
+    add_outer2<T, D>(dq, pk, keys, row0, dp, s, ln);
+    feed<T, D / 16, 2, 2>();
+  } else {
+    add_outer<T, D>(dq, keys, row0, dp, ln);
+  }
+}
 template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
 __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8) ? 2 : 1) k_forms_bwd_q(FormArgs a) {
   using Q = BwdQ<T, D, FEW, NW>;
@@ -920,7 +950,6 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   const RowOf r = row_of(a, Rw + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, Q::ROWS, prefix, wave, lane);
   const Score sc = make_score<CAP>(a.scale, a.cap);
-  const float factor = score_factor<CAP, SLOPES>(sc);
   const Lane<T, D> ln(lane);
   typename Q::Keys kv;
   kv.init(a, b, hk, lds, tid);
@@ -946,7 +975,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   }
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
 
-  f32x16_t dq[D / 32], pk[MEND ? D / 32 : 1], damp;
+  f32x16_t dq[D / 32], pk[MEND ? D / 32 : 1];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = zero16();
 #pragma unroll
@@ -969,28 +998,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
 #pragma unroll Q::SPARE ? 1 : NK
       for (int kb = 0; kb < NK; ++kb) {
         const int row0 = 32 * (FEW ? wave : kb);
-        f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln), dp;
-        if constexpr (Q::SPARE) dp = dot_tiles<T, D>(kv.values(i), row0, lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln);
-        else dp = dot_rows<T, D>(kv.values(i), row0, gf, ln);
-        feed<T, Tile<T, D>::NS, 1, 1>();
-        feed<T, Tile<T, D>::NS, Q::SPARE ? 2 : 1, 1>();
-        scores<CAP, SLOPES, true>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, damp);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
-          if constexpr (MEND) rest += ds;
-          if constexpr (CAP) {
-            ds *= damp[j];
-            p *= damp[j];
-          }
-          s[j] = p;
-          dp[j] = ds;
-        }
-        if constexpr (MEND) {
-          add_outer2<T, D>(dq, pk, kv.keys(i), row0, dp, s, ln);
-          feed<T, D / 16, 2, 2>();
-        }
-        else add_outer<T, D>(dq, kv.keys(i), row0, dp, ln);
+        query_block<T, D, CAP, SLOPES, MEND, Q::SPARE>(a, sc, r, kv.keys(i), kv.values(i), row0, kv.ids(i) + row0, k0 + row0, ws.lim_lo, state == 1, qf, gf,
+                                                       lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln, half, l2, delta, dq, pk, rest);
       }
     }
   }
@@ -1033,6 +1042,80 @@ __device__ __forceinline__ f32x16_t rows_of(const float* x, int half) {
 }
 
 // ---- backward, key side: dK, dV ---------------------------------------------------------------------------------------
+// What the key side has to know of the rows of a tile.
+template <int RT>
+struct RowsMeta {
+  float l2[RT], delta[RT], slope[RT];        // -log-sum-exp in base 2 (no cap, no slopes: over the score's factor), -delta
+  int lim[RT], id[RT], pos[RT];
+  template <bool PLAIN>
+  __device__ __forceinline__ void put(int i, const RowOf& r, const Score& sc, float lse, float d) {
+    l2[i] = lse == -INFINITY ? -INFINITY : -lse * (PLAIN ? LOG2E / sc.a : LOG2E);     // rows that see nothing: probabilities zero
+    delta[i] = -d;
+    slope[i] = r.slope2;
+    lim[i] = r.lim;
+    id[i] = r.id;
+    pos[i] = r.pos;
+  }
+};
+// A wavefront's 32 keys (key: the lane's) and the rows 32 rb .. of the tiles of queries and of output gradients: dK, dV grow.
+template <typename T, int D, bool CAP, bool SLOPES, bool SPARE, int RT>
+__device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m, uint32_t queries, uint32_t grads, int rb, const Frags<T, D>& kf,
+                                          const Frags<T, D>& vf, uint32_t keys, uint32_t values, int key, int kid, bool mask, const Lane<T, D>& ln,
+                                          int half, f32x16_t (&dk)[D / 32], f32x16_t (&dv)[D / 32]) {
+  constexpr bool PLAIN = !CAP && !SLOPES;
+  // without cap and slopes the products start from what is taken off them, the row's log-sum-exp and delta
+  f32x16_t s = PLAIN ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
+  if constexpr (SPARE) {
+    s = dot_tiles<T, D>(queries, 32 * rb, keys, ln, s);
+    dp = dot_tiles<T, D>(grads, 32 * rb, values, ln, dp);
+  } else {
+    s = dot_rows<T, D>(queries, 32 * rb, kf, ln, s);
+    dp = dot_rows<T, D>(grads, 32 * rb, vf, ln, dp);
+  }
+  feed<T, Tile<T, D>::NS, SPARE ? 2 : 1, 1>();
+  feed<T, Tile<T, D>::NS, SPARE ? 2 : 1, 1>();
+  f32x16_t damp;
+  if constexpr (CAP) cap_scores<true>(sc, s, damp);
+  if constexpr (SLOPES) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int at4 = 32 * rb + 8 * g + 4 * half;
+      const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
+      const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
+      const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), (CAP ? 1.f : sc.a) * s[4 * g + j]);
+    }
+  }
+  if (mask) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int at4 = 32 * rb + 8 * g + 4 * half;
+      const int4 lm = *reinterpret_cast<const int4*>(m.lim + at4), qi = *reinterpret_cast<const int4*>(m.id + at4);
+      const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * g + j] = key < lim[j] & (qid[j] == kid) ? s[4 * g + j] : -INFINITY;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    f32x4_t l2 = f32x4_t{0.f, 0.f, 0.f, 0.f}, dl = l2;
+    if constexpr (!PLAIN) {
+      l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
+      dl = *reinterpret_cast<const f32x4_t*>(m.delta + 32 * rb + 8 * g + 4 * half);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float p = __builtin_amdgcn_exp2f(PLAIN ? sc.a * s[4 * g + j] : s[4 * g + j] + l2[j]);
+      s[4 * g + j] = p;
+      dp[4 * g + j] = p * (PLAIN ? dp[4 * g + j] : dp[4 * g + j] + dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
+    }
+  }
+  add_outer<T, D>(dv, grads, 32 * rb, s, ln);
+  add_outer<T, D>(dk, queries, 32 * rb, dp, ln);
+  feed<T, D / 8, 2, 1>();
+}
+
 // BLOCKS times 32 keys, over tiles of as many queries as have their rows (one for each of the G heads of the group) in RT.
 // BLOCKS wavefronts take 32 keys each; where there are more, they share the rows of a tile and add up at the end:
 //   4 of 4: 128 keys, tiles of 64 rows.  4 of 8 (bf16 at width 128): the same, two wavefronts to 32 keys; keys and values stay in
@@ -1044,10 +1127,7 @@ struct BwdKv {
   static constexpr int BUFS = TILE > 32768 ? 1 : 2;
   static constexpr bool SPARE = NW == 8;
   static constexpr int LDS = BUFS * STAGE + (SPARE ? 2 * 128 * Tile<T, D>::ROWB : 0);
-  struct Meta {
-    float l2[RT], delta[RT], slope[RT];        // -log-sum-exp in base 2 (PLAIN: over the score's factor), -delta
-    int lim[RT], id[RT], pos[RT];
-  };
+  using Meta = RowsMeta<RT>;
   static_assert(BUFS * STAGE >= (PARTS - 1) * BLOCKS * 32 * D * 4, "the sums' room");
 };
 template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW>
@@ -1119,13 +1199,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
   };
   auto commit = [&](int i) {
     if (tid >= RT) return;
-    typename K::Meta& m = meta[i & (K::BUFS - 1)];
-    m.l2[tid] = ml2 == -INFINITY ? -INFINITY : -ml2 * (PLAIN ? LOG2E / sc.a : LOG2E);     // rows that see nothing: probabilities zero
-    m.delta[tid] = -mdelta;
-    m.slope[tid] = mr.slope2;
-    m.lim[tid] = mr.lim;
-    m.id[tid] = mr.id;
-    m.pos[tid] = mr.pos;
+    meta[i & (K::BUFS - 1)].template put<PLAIN>(tid, mr, sc, ml2, mdelta);
   };
 
   const int all_tiles = (a.n + QT - 1) / QT, n_tiles = (all_tiles - split + a.row_splits - 1) / a.row_splits;   // every row_splits-th
@@ -1161,57 +1235,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8
       if (!hidden) {
 #pragma unroll 1
         for (int rb = part * NR; rb < part * NR + NR; ++rb) {
-          // without cap and slopes the products start from what is taken off them, the row's log-sum-exp and delta
-          f32x16_t s = PLAIN ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
-          if constexpr (K::SPARE) {
-            s = dot_tiles<T, D>(tile, 32 * rb, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB, ln, s);
-            dp = dot_tiles<T, D>(tile + TILE, 32 * rb, lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, ln, dp);
-          } else {
-            s = dot_rows<T, D>(tile, 32 * rb, kf, ln, s);
-            dp = dot_rows<T, D>(tile + TILE, 32 * rb, vf, ln, dp);
-          }
-          feed<T, Tile<T, D>::NS, K::SPARE ? 2 : 1, 1>();
-          feed<T, Tile<T, D>::NS, K::SPARE ? 2 : 1, 1>();
-          f32x16_t damp;
-          if constexpr (CAP) cap_scores<true>(sc, s, damp);
-          if constexpr (SLOPES) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const int at4 = 32 * rb + 8 * g + 4 * half;
-              const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
-              const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
-              const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), (CAP ? 1.f : sc.a) * s[4 * g + j]);
-            }
-          }
-          if (mask) {
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-              const int at4 = 32 * rb + 8 * g + 4 * half;
-              const int4 lm = *reinterpret_cast<const int4*>(m.lim + at4), qi = *reinterpret_cast<const int4*>(m.id + at4);
-              const int lim[4] = {lm.x, lm.y, lm.z, lm.w}, qid[4] = {qi.x, qi.y, qi.z, qi.w};
-#pragma unroll
-              for (int j = 0; j < 4; ++j) s[4 * g + j] = key < lim[j] & (qid[j] == kid) ? s[4 * g + j] : -INFINITY;
-            }
-          }
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            f32x4_t l2 = f32x4_t{0.f, 0.f, 0.f, 0.f}, dl = l2;
-            if constexpr (!PLAIN) {
-              l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
-              dl = *reinterpret_cast<const f32x4_t*>(m.delta + 32 * rb + 8 * g + 4 * half);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float p = __builtin_amdgcn_exp2f(PLAIN ? sc.a * s[4 * g + j] : s[4 * g + j] + l2[j]);
-              s[4 * g + j] = p;
-              dp[4 * g + j] = p * (PLAIN ? dp[4 * g + j] : dp[4 * g + j] + dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
-            }
-          }
-          add_outer<T, D>(dv, tile + TILE, 32 * rb, s, ln);
-          add_outer<T, D>(dk, tile, 32 * rb, dp, ln);
-          feed<T, D / 8, 2, 1>();
+          key_block<T, D, CAP, SLOPES, K::SPARE>(sc, m, tile, tile + TILE, rb, kf, vf, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB,
+                                                 lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, key, kid, mask, ln, half, dk, dv);
         }
       }
       if (K::BUFS > 1 && i + 1 < count) commit(i + 1);
@@ -1246,6 +1271,118 @@ __global__ void __launch_bounds__(256) k_forms_kv_join(FormArgs a) {
   const int d = (int)(i % a.w), key = (int)(row % a.S), hk = (int)(row / a.S) % a.nkv, b = (int)(row / ((size_t)a.S * a.nkv));
   const FormHeads& out = v ? a.dv : a.dk;
   store4(head_out<T>(out, b, hk) + (long long)key * out.sr + d, x[0], x[1], x[2], x[3]);
+}
+
+// ---- backward of short sequences --------------------------------------------------------------------------------------
+// Both sides at once where a head's keys and the rows that see them fit a tile each: queries, output gradients, keys and values of
+// a kv head are read once, where the two kernels read them twice, and the two sides' launch and first loads are paid for once.  Each
+// wavefront works on 32 rows over all keys, hands on log-sum-exp and delta through LDS, then on 32 keys over all rows.
+// Bound by memory: 64x128x16 heads of 64 move 134 MB.
+constexpr int ONE = 128;
+template <typename T, int D>
+struct BwdOne {
+  static constexpr int TILE = ONE * Tile<T, D>::ROWB, LDS = 4 * TILE + TILE_ALIGN;
+};
+template <typename T, int D, bool CAP, bool SLOPES>
+__global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
+  static_assert(sizeof(T) == 2 && ONE * 4 <= TILE_ALIGN, "two workgroups share the LDS of a compute unit");
+  constexpr int TILE = BwdOne<T, D>::TILE;
+  constexpr bool PLAIN = !CAP && !SLOPES;
+  extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
+  __shared__ int2 ranges_s[FORM_OWN_RANGES];
+  __shared__ __attribute__((aligned(16))) RowsMeta<ONE> m;
+  const uint32_t Qs = lds_addr(lds), Gs = Qs + TILE, Ks = Gs + TILE, Vs = Ks + TILE;
+  int* const ids = reinterpret_cast<int*>(lds + 4 * TILE);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+  const int G = a.nh / a.nkv, rows = a.n * G, first = a.S - a.n, hk = blockIdx.x % a.nkv, b = blockIdx.x / a.nkv;
+  const int prefix = a.prefix ? a.prefix[b] : 0;
+  const int32_t* docs = a.docs ? a.docs + (size_t)b * a.S : nullptr;
+  const int own = wave * 32 + (lane & 31);                                // the lane's row, then its key
+
+  const RowOf r = row_of(a, own, b, hk, prefix);
+  {
+    Loader<T, D, ONE, 4> x;
+    auto seen = [&](int at) { return docs == nullptr || docs[at] >= 0; };
+    auto row = [&](int i) { return i < rows && seen(first + i / G); };
+    auto key = [&](int i) { return i < a.S && seen(i); };
+    x.init(tid, a.q.sr * (int)sizeof(T), G, a.q.sh * (int)sizeof(T), rows, a.w);
+    x.issue(head_ptr<T>(a.q, b, hk * G), Qs, tid, true, row);
+    x.init(tid, a.k.sr * (int)sizeof(T), 1, 0, a.S, a.w);
+    x.issue(head_ptr<T>(a.k, b, hk), Ks, tid, true, key);
+    x.init(tid, a.v.sr * (int)sizeof(T), 1, 0, a.S, a.w);
+    x.issue(head_ptr<T>(a.v, b, hk), Vs, tid, true, key);
+    x.init(tid, a.g.sr * (int)sizeof(T), G, a.g.sh * (int)sizeof(T), rows, a.w);
+    x.issue(head_ptr<T>(a.g, b, hk * G), Gs, tid, true, row);
+  }
+  Frags<T, D> qf, gf, of;
+  load_frags<T, D>(of, head_ptr<T>(a.o, b, r.head) + (long long)r.qi * a.o.sr, half, a.w, r.live);
+  const size_t lrow = ((size_t)b * a.nh + r.head) * a.n + r.qi;
+  const float lse = r.live ? a.lse[lrow] : -INFINITY;
+  const float l2 = lse == -INFINITY ? INFINITY : lse * LOG2E;             // sees no key: probabilities zero
+  const bool in = own < a.S;
+  const int kid = docs ? (in ? docs[own] : -1) : 0;
+  const bool live = in && kid >= 0;
+  if (half == 0) ids[own] = kid;
+  const int2* ranges = doc_ranges(a, b, ranges_s, tid, 256);
+  const int Rw = __builtin_amdgcn_readfirstlane(wave * 32);
+  const Span ws = wave_span(a, r, Rw, prefix);
+  const int kid_lo = wave_min_i(live ? kid : 0x7fffffff), kid_hi = wave_max_i(live ? kid : -1);
+  const Score sc = make_score<CAP>(a.scale, a.cap);
+  const Lane<T, D> ln(lane);
+  float delta = 0.f, rest = 0.f;
+  __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): the entries
+  landed<0, 2>(0);
+#pragma unroll
+  for (int s = 0; s < Tile<T, D>::NS; ++s) {
+    qf[s] = *Tile<T, D>::at(lds, own, 2 * s + half);
+    gf[s] = *Tile<T, D>::at(lds + TILE, own, 2 * s + half);
+    delta += dot_chunk<T>(gf[s], of[s]);
+  }
+  delta += __shfl_xor(delta, 32, 64);
+
+  {
+    f32x16_t dq[D / 32], pk[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) dq[i] = pk[i] = zero16();
+#pragma unroll 1
+    for (int k0 = 0; k0 < a.S; k0 += 32) {
+      int lo, hi;
+      positions_range(ranges, k0, k0, lo, hi);
+      const int state = tile_state(a, ws, k0, 32, lo, hi);
+      if (state == 0) continue;
+      query_block<T, D, CAP, SLOPES, true, false>(a, sc, r, Ks, Vs, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
+    }
+    rest += __shfl_xor(rest, 32, 64);
+    delta += rest;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
+    if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
+  }
+  if (half == 0) m.template put<PLAIN>(own, r, sc, lse, r.live ? delta : 0.f);
+  __syncthreads();
+
+#pragma unroll
+  for (int s = 0; s < Tile<T, D>::NS; ++s) {
+    qf[s] = *Tile<T, D>::at(lds + 2 * TILE, own, 2 * s + half);           // the lane's key and value
+    gf[s] = *Tile<T, D>::at(lds + 3 * TILE, own, 2 * s + half);
+  }
+  f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
+#pragma unroll 1
+  for (int R0 = 0; R0 < rows; R0 += 32) {
+    const int p0 = first + R0 / G, p1 = first + (min(rows, R0 + 32) - 1) / G;
+    int lo, hi;
+    positions_range(ranges, p0, p1, lo, hi);
+    if (Rw >= key_limit(a, p1, prefix) || kid_hi < 0 || (docs && (hi < kid_lo || lo > kid_hi))) continue;
+    const bool mask = Rw + 32 > key_limit(a, p0, prefix) || (docs && !(lo == hi && lo == kid_lo && lo == kid_hi));
+    key_block<T, D, CAP, SLOPES, false>(sc, m, Qs, Gs, R0 / 32, qf, gf, 0, 0, own, kid, mask, ln, half, dk, dv);
+  }
+  if (!in) return;
+  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, a.scale, live);
+  store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)own * a.dv.sr, dv, half, a.w, 1.f, live);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
@@ -1291,6 +1428,8 @@ struct Launch {
   static hipError_t bwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv;
+    if constexpr (sizeof(T) == 2 && D == 64)
+      if (a.S <= ONE && rows <= ONE) return launch<k_forms_bwd_one<T, D, CAP, SLOPES>>(256, heads, BwdOne<T, D>::LDS, a, s);
     const RowMode mode = row_mode(WIDE, D, heads, rows);
     hipError_t e;
     if (mode == ROWS_FEW) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, true, 4>>(256, heads * tiles(rows, 32), BwdQ<T, D, true, 4>::LDS, a, s);

@@ -81,6 +81,14 @@ def test_attention_against_the_definition(shape, form, dtype):
     _case(torch, getattr(torch, dtype), *shape, seed=form, **FORMS[form])
 
 
+@pytest.mark.parametrize("form", range(len(FORMS)))
+@pytest.mark.parametrize("shape", [(3, 40, 100, 6, 2, 48), (2, 64, 64, 4, 2, 64), (1, 32, 128, 4, 1, 40), (2, 1, 128, 128, 2, 64), (5, 128, 128, 3, 3, 64),
+                                   (2, 97, 127, 2, 2, 56)], ids=lambda s: "x".join(map(str, s)))
+def test_short_sequences(shape, form):
+    import torch
+    _case(torch, torch.bfloat16, *shape, **FORMS[form], seed=3)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("form", [0, 5, 6])
 @pytest.mark.parametrize("shape", [(32, 128, 128, 8, 8, 64), (40, 200, 200, 8, 8, 64), (64, 256, 256, 4, 4, 128), (70, 330, 350, 8, 4, 96),
