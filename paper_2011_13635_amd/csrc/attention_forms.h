@@ -1274,25 +1274,27 @@ __global__ void __launch_bounds__(256) k_forms_kv_join(FormArgs a) {
 }
 
 // ---- backward of short sequences --------------------------------------------------------------------------------------
-// Both sides at once where a head's keys and the rows that see them fit a tile each: queries, output gradients, keys and values of
-// a kv head are read once, where the two kernels read them twice, and the two sides' launch and first loads are paid for once.  Each
-// wavefront works on 32 rows over all keys, hands on log-sum-exp and delta through LDS, then on 32 keys over all rows.
-// Bound by memory: 64x128x16 heads of 64 move 134 MB.
+// Both sides at once where a head's keys and the rows that see them fit a tile each: every operand is read once, where the two
+// kernels read queries, keys, values and output gradients twice, and the two sides' launch and first loads are paid for once.  Each
+// wavefront works on 32 rows over all keys, then on 32 keys over all rows; between the two the rows' queries and gradients go from
+// registers into the tiles of the keys and values, whose own go into registers.
+// 64x128x16 heads of 64, 134 MB: 52 us against 67 of the two kernels.  Its loads and stores alone take 33, each side's products 10
+// more: the registers hold two wavefronts a SIMD, too few for loads and products to overlap.  Three, of 168 registers, spill: 54.
 constexpr int ONE = 128;
 template <typename T, int D>
 struct BwdOne {
-  static constexpr int TILE = ONE * Tile<T, D>::ROWB, LDS = 4 * TILE + TILE_ALIGN;
+  static constexpr int TILE = ONE * Tile<T, D>::ROWB, LDS = 2 * TILE + TILE_ALIGN;
 };
 template <typename T, int D, bool CAP, bool SLOPES>
 __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
-  static_assert(sizeof(T) == 2 && ONE * 4 <= TILE_ALIGN, "two workgroups share the LDS of a compute unit");
+  static_assert(sizeof(T) == 2 && ONE * 4 <= TILE_ALIGN, "the entries' room");
   constexpr int TILE = BwdOne<T, D>::TILE;
   constexpr bool PLAIN = !CAP && !SLOPES;
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ __attribute__((aligned(16))) RowsMeta<ONE> m;
-  const uint32_t Qs = lds_addr(lds), Gs = Qs + TILE, Ks = Gs + TILE, Vs = Ks + TILE;
-  int* const ids = reinterpret_cast<int*>(lds + 4 * TILE);
+  const uint32_t first_tile = lds_addr(lds), second_tile = first_tile + TILE;      // keys and values, then queries and gradients
+  int* const ids = reinterpret_cast<int*>(lds + 2 * TILE);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int G = a.nh / a.nkv, rows = a.n * G, first = a.S - a.n, hk = blockIdx.x % a.nkv, b = blockIdx.x / a.nkv;
   const int prefix = a.prefix ? a.prefix[b] : 0;
@@ -1302,19 +1304,15 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
   const RowOf r = row_of(a, own, b, hk, prefix);
   {
     Loader<T, D, ONE, 4> x;
-    auto seen = [&](int at) { return docs == nullptr || docs[at] >= 0; };
-    auto row = [&](int i) { return i < rows && seen(first + i / G); };
-    auto key = [&](int i) { return i < a.S && seen(i); };
-    x.init(tid, a.q.sr * (int)sizeof(T), G, a.q.sh * (int)sizeof(T), rows, a.w);
-    x.issue(head_ptr<T>(a.q, b, hk * G), Qs, tid, true, row);
+    auto key = [&](int i) { return i < a.S && (docs == nullptr || docs[i] >= 0); };
     x.init(tid, a.k.sr * (int)sizeof(T), 1, 0, a.S, a.w);
-    x.issue(head_ptr<T>(a.k, b, hk), Ks, tid, true, key);
+    x.issue(head_ptr<T>(a.k, b, hk), first_tile, tid, true, key);
     x.init(tid, a.v.sr * (int)sizeof(T), 1, 0, a.S, a.w);
-    x.issue(head_ptr<T>(a.v, b, hk), Vs, tid, true, key);
-    x.init(tid, a.g.sr * (int)sizeof(T), G, a.g.sh * (int)sizeof(T), rows, a.w);
-    x.issue(head_ptr<T>(a.g, b, hk * G), Gs, tid, true, row);
+    x.issue(head_ptr<T>(a.v, b, hk), second_tile, tid, true, key);
   }
   Frags<T, D> qf, gf, of;
+  load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
+  load_frags<T, D>(gf, head_ptr<T>(a.g, b, r.head) + (long long)r.qi * a.g.sr, half, a.w, r.live);
   load_frags<T, D>(of, head_ptr<T>(a.o, b, r.head) + (long long)r.qi * a.o.sr, half, a.w, r.live);
   const size_t lrow = ((size_t)b * a.nh + r.head) * a.n + r.qi;
   const float lse = r.live ? a.lse[lrow] : -INFINITY;
@@ -1333,11 +1331,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
   __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): the entries
   landed<0, 2>(0);
 #pragma unroll
-  for (int s = 0; s < Tile<T, D>::NS; ++s) {
-    qf[s] = *Tile<T, D>::at(lds, own, 2 * s + half);
-    gf[s] = *Tile<T, D>::at(lds + TILE, own, 2 * s + half);
-    delta += dot_chunk<T>(gf[s], of[s]);
-  }
+  for (int s = 0; s < Tile<T, D>::NS; ++s) delta += dot_chunk<T>(gf[s], of[s]);
   delta += __shfl_xor(delta, 32, 64);
 
   {
@@ -1350,7 +1344,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
       positions_range(ranges, k0, k0, lo, hi);
       const int state = tile_state(a, ws, k0, 32, lo, hi);
       if (state == 0) continue;
-      query_block<T, D, CAP, SLOPES, true, false>(a, sc, r, Ks, Vs, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
+      query_block<T, D, CAP, SLOPES, true, false>(a, sc, r, first_tile, second_tile, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
     }
     rest += __shfl_xor(rest, 32, 64);
     delta += rest;
@@ -1361,13 +1355,20 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
     if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
   }
   if (half == 0) m.template put<PLAIN>(own, r, sc, lse, r.live ? delta : 0.f);
-  __syncthreads();
 
+  Frags<T, D> kf, vf;      // of the lane's key
 #pragma unroll
   for (int s = 0; s < Tile<T, D>::NS; ++s) {
-    qf[s] = *Tile<T, D>::at(lds + 2 * TILE, own, 2 * s + half);           // the lane's key and value
-    gf[s] = *Tile<T, D>::at(lds + 3 * TILE, own, 2 * s + half);
+    kf[s] = *Tile<T, D>::at(lds, own, 2 * s + half);
+    vf[s] = *Tile<T, D>::at(lds + TILE, own, 2 * s + half);
   }
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < Tile<T, D>::NS; ++s) {
+    *Tile<T, D>::at(lds, own, 2 * s + half) = qf[s];
+    *Tile<T, D>::at(lds + TILE, own, 2 * s + half) = gf[s];
+  }
+  __syncthreads();
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zero16();
@@ -1378,7 +1379,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
     positions_range(ranges, p0, p1, lo, hi);
     if (Rw >= key_limit(a, p1, prefix) || kid_hi < 0 || (docs && (hi < kid_lo || lo > kid_hi))) continue;
     const bool mask = Rw + 32 > key_limit(a, p0, prefix) || (docs && !(lo == hi && lo == kid_lo && lo == kid_hi));
-    key_block<T, D, CAP, SLOPES, false>(sc, m, Qs, Gs, R0 / 32, qf, gf, 0, 0, own, kid, mask, ln, half, dk, dv);
+    key_block<T, D, CAP, SLOPES, false>(sc, m, first_tile, second_tile, R0 / 32, kf, vf, 0, 0, own, kid, mask, ln, half, dk, dv);
   }
   if (!in) return;
   store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, a.scale, live);
