@@ -633,7 +633,11 @@ struct KeyTiles {
 // Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
 template <typename T, int D, bool CAP, bool FEW, int NW>
 struct Fwd {
-  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB, STAGES = TILE > 32768 ? 1 : 2;
+  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB;
+  // One stage where two would leave room for one workgroup of a compute unit (bf16 at width 128, 8x1 queries over 8191 keys: 32.6
+  // -> 29.5 us, 2x512x16 heads 21.1 -> 15.6; with a single workgroup to each, 1x1024x8 heads, 16.7 -> 17.5).  fp32 has the registers
+  // for one only (4x1024x8 heads: 144 -> 147).
+  static constexpr int STAGES = TILE > (sizeof(T) == 2 ? 32767 : 32768) ? 1 : 2;
   // wavefronts that share a SIMD: as many as the registers of the accumulators allow
   static constexpr int WAVES = sizeof(T) == 4 ? 1 : D == 64 && !FEW ? (CAP ? 3 : 4) : 2;
   using Keys = KeyTiles<T, D, KT, STAGES, NW>;
