@@ -271,19 +271,23 @@ __device__ __forceinline__ void cap_scores(const Score& f, f32x16_t& s, f32x16_t
   }
 }
 
-// Least and largest document entry of every 64 positions of a sequence.  Up to 64 such blocks a workgroup finds them itself, one
-// wavefront a block (a launch of its own takes longer); beyond that k_doc_ranges has.  Called by the whole workgroup.
-__device__ __forceinline__ const int2* doc_ranges(const FormArgs& a, int b, int2 (&room)[FORM_OWN_RANGES], int tid, int threads) {
+// Least and largest document entry of every 64 positions of a sequence, of which a workgroup needs `most` from block `from` on.  Up
+// to 64 it finds them itself, one wavefront a block (a launch of its own takes longer); beyond that k_doc_ranges has.  Called by the
+// whole workgroup.
+__device__ __forceinline__ const int2* doc_ranges(const FormArgs& a, int b, int2 (&room)[FORM_OWN_RANGES], int tid, int threads, int from, int most) {
   const int blocks = (a.S + 63) / 64;
   if (!a.docs) return nullptr;
-  if (blocks > FORM_OWN_RANGES) return a.ranges + (size_t)b * blocks;
-  for (int i = tid >> 6; i < blocks; i += threads >> 6) {
-    const int v = a.docs[(size_t)b * a.S + min(64 * i + (tid & 63), a.S - 1)];
+  if (most > FORM_OWN_RANGES) return a.ranges + (size_t)b * blocks;
+  for (int i = tid >> 6; i < min(most, blocks - from); i += threads >> 6) {
+    const int v = a.docs[(size_t)b * a.S + min(64 * (from + i) + (tid & 63), a.S - 1)];
     const int lo = wave_min_i(v), hi = wave_max_i(v);
     if ((tid & 63) == 0) room[i] = make_int2(lo, hi);
   }
   __syncthreads();
-  return room;
+  return room - from;
+}
+__device__ __forceinline__ const int2* doc_ranges(const FormArgs& a, int b, int2 (&room)[FORM_OWN_RANGES], int tid, int threads) {
+  return doc_ranges(a, b, room, tid, threads, 0, (a.S + 63) / 64);
 }
 
 // Which tile of which kv head a workgroup takes.  Workgroups go round the eight XCDs; the tiles of one kv head are given to one
@@ -675,7 +679,8 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
   const int hk = bh % a.nkv, b = bh / a.nkv;
 
   const int prefix = a.prefix ? a.prefix[b] : 0;
-  const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW);
+  const int n_tiles = (a.S + F::KT - 1) / F::KT, per = (n_tiles + a.splits - 1) / a.splits;
+  const int2* ranges = doc_ranges(a, b, ranges_s, tid, 64 * NW, split * per * (F::KT / 64), per * (F::KT / 64));
   const int R0 = rt * F::ROWS, Rw = __builtin_amdgcn_readfirstlane(R0 + (FEW ? 0 : wave * 32));
   const RowOf r = row_of(a, Rw + (lane & 31), b, hk, prefix);
   const Span ws = wave_span(a, r, Rw, prefix), gs = group_span<NW>(a, ws, span_s, R0, F::ROWS, prefix, wave, lane);
@@ -712,7 +717,6 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
     }
     l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   };
-  const int n_tiles = (a.S + F::KT - 1) / F::KT, per = (n_tiles + a.splits - 1) / a.splits;
   const int t_end = min(n_tiles, (split + 1) * per);
   for (int base = split * per; base < t_end; base += LIST) {
     const int t = base + tid;

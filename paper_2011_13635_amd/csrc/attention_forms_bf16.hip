@@ -14,7 +14,9 @@ __global__ void __launch_bounds__(256) k_doc_ranges(const int32_t* __restrict__ 
   if (lane == 0) ranges[i] = make_int2(lo, hi);
 }
 hipError_t form_ranges(const FormArgs& a, hipStream_t s) {
-  if (!a.docs || (a.S + 63) / 64 <= FORM_OWN_RANGES) return hipSuccess;
+  // a workgroup's share: where keys are split, whole tiles of 128
+  const int most = a.splits > 1 ? 2 * (((a.S + 127) / 128 + a.splits - 1) / a.splits) : (a.S + 63) / 64;
+  if (!a.docs || most <= FORM_OWN_RANGES) return hipSuccess;
   const long long blocks = (long long)a.B * ((a.S + 63) / 64);
   k_doc_ranges<<<dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, s>>>(a.docs, a.ranges, a.B, a.S);
   return hipGetLastError();
