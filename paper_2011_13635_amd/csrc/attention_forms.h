@@ -647,13 +647,14 @@ struct KeyTiles {
 // Few workgroups: the keys are split over a.splits workgroups whose results k_forms_join puts together.
 template <typename T, int D, bool CAP, bool FEW, int NW>
 struct Fwd {
+  static constexpr bool WIDE32 = sizeof(T) == 4 && D == 128;
   static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB;
   // One stage where two would leave room for one workgroup of a compute unit (bf16 at width 128, 8x1 queries over 8191 keys: 32.6
-  // -> 29.5 us, 2x512x16 heads 21.1 -> 15.6; with a single workgroup to each, 1x1024x8 heads, 16.7 -> 17.5).  fp32 has the registers
-  // for one only (4x1024x8 heads: 144 -> 147).
-  static constexpr int STAGES = TILE > (sizeof(T) == 2 ? 32767 : 32768) ? 1 : 2;
-  // wavefronts that share a SIMD: as many as the registers of the accumulators allow
-  static constexpr int WAVES = sizeof(T) == 4 ? 1 : D == 64 && !FEW ? (CAP ? 3 : 4) : 2;
+  // -> 29.5 us, 2x512x16 heads 21.1 -> 15.6; with a single workgroup to each, 1x1024x8 heads, 16.7 -> 17.5) and the registers do not.
+  static constexpr int STAGES = TILE > (WIDE32 ? 32768 : 32767) ? 1 : 2;
+  // Wavefronts that share a SIMD: as many as the registers of the accumulators allow (fp32 at width 64, 4x1024x8 heads: 144 us with
+  // one, 97 with two; 3x203x12 16.0, 13.5).
+  static constexpr int WAVES = WIDE32 ? 1 : sizeof(T) == 2 && D == 64 && !FEW ? (CAP ? 3 : 4) : 2;
   using Keys = KeyTiles<T, D, KT, STAGES, NW>;
   static constexpr int JOIN = FEW ? 4 * 32 * (D + 4) * 4 + 2 * 4 * 32 * 4 : 0;
   static constexpr int LDS = Keys::LDS > JOIN ? Keys::LDS : JOIN;
@@ -911,7 +912,9 @@ __device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
 // FEW as in the forward.
 template <typename T, int D, bool FEW, int NW>
 struct BwdQ {
-  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB, STAGES = TILE > 32768 ? 1 : 2;
+  static constexpr int KT = FEW ? 128 : 64, ROWS = FEW ? 32 : 32 * NW, TILE = KT * Tile<T, D>::ROWB;
+  // wavefronts that share a SIMD (fp32 at width 64, 4x1024x8 heads, both sides: 414 us with one, 369 with two here)
+  static constexpr int WAVES = D == 64 || NW == 8 ? 2 : 1, STAGES = TILE > (sizeof(T) == 4 && D == 64 ? 32767 : 32768) ? 1 : 2;
   static constexpr bool MEND = sizeof(T) == 2, SPARE = sizeof(T) == 2 && D == 128;
   using Keys = KeyTiles<T, D, KT, STAGES, NW>;
   static constexpr int LDS = Keys::LDS + (SPARE ? ROWS * Tile<T, D>::ROWB : 0);
@@ -948,7 +951,7 @@ __device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, 
   }
 }
 template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8) ? 2 : 1) k_forms_bwd_q(FormArgs a) {
+__global__ void __launch_bounds__(64 * NW, (BwdQ<T, D, FEW, NW>::WAVES)) k_forms_bwd_q(FormArgs a) {
   fetch_args(a);
   using Q = BwdQ<T, D, FEW, NW>;
   static_assert(!FEW || NW == 4, "the wavefronts that share 32 rows");
@@ -1142,19 +1145,22 @@ __device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m
 //   4 of 4: 128 keys, tiles of 64 rows.  4 of 8 (bf16 at width 128): the same, two wavefronts to 32 keys; keys and values stay in
 //   LDS, as the accumulators fill the registers.  1 of 4 (few keys in all): 32 keys, tiles of 128 rows.
 // Few workgroups: the rows are split over a.row_splits workgroups, whose sums k_forms_kv_join adds.
-template <typename T, int D, int BLOCKS, int NW>
+// Wavefronts that share a SIMD: two at width 64, and of a workgroup of eight.  fp32 at width 64: two cost spilled registers, and the
+// second stage of the tiles, and pay only where there are workgroups for them (4x1024x8 heads, both sides: 369 us with one, 322 with
+// two; 1x512x12 heads, 192 workgroups: 60 and 65).
+template <typename T, int D, int BLOCKS, int NW, int WAVES>
 struct BwdKv {
   static constexpr int PARTS = NW / BLOCKS, RT = PARTS == 4 ? 128 : 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
-  static constexpr int BUFS = TILE > 32768 ? 1 : 2;
+  static constexpr int BUFS = TILE > (NW == 4 && WAVES == 2 ? 32767 : 32768) ? 1 : 2;
   static constexpr bool SPARE = NW == 8;
   static constexpr int LDS = BUFS * STAGE + (SPARE ? 2 * 128 * Tile<T, D>::ROWB : 0);
   using Meta = RowsMeta<RT>;
   static_assert(BUFS * STAGE >= (PARTS - 1) * BLOCKS * 32 * D * 4, "the sums' room");
 };
-template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && (D == 64 || NW == 8) ? 2 : 1) k_forms_bwd_kv(FormArgs a) {
+template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW, int WAVES>
+__global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
   fetch_args(a);
-  using K = BwdKv<T, D, BLOCKS, NW>;
+  using K = BwdKv<T, D, BLOCKS, NW, WAVES>;
   constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;
   constexpr bool PLAIN = !CAP && !SLOPES;  // NR: blocks of 32 rows of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
@@ -1449,6 +1455,16 @@ struct Launch {
     if (e != hipSuccess || a.splits == 1) return e;
     return launch<k_forms_join<T>>(256, (heads * rows + 3) / 4, 0, a, s);
   }
+  template <int BLOCKS, int WAVEFRONTS, int WAVES>
+  static hipError_t key_side_of(const FormArgs& a, size_t blocks, hipStream_t s) {
+    return launch<k_forms_bwd_kv<T, D, CAP, SLOPES, BLOCKS, WAVEFRONTS, WAVES>>(64 * WAVEFRONTS, blocks, BwdKv<T, D, BLOCKS, WAVEFRONTS, WAVES>::LDS, a, s);
+  }
+  template <int BLOCKS, int WAVEFRONTS>
+  static hipError_t key_side(const FormArgs& a, size_t blocks, hipStream_t s) {
+    if constexpr (sizeof(T) == 4 && D == 64 && BLOCKS == 1)
+      if (blocks <= 256) return key_side_of<BLOCKS, WAVEFRONTS, 1>(a, blocks, s);
+    return key_side_of<BLOCKS, WAVEFRONTS, D == 64 || WAVEFRONTS == 8 ? 2 : 1>(a, blocks, s);
+  }
   static hipError_t bwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv;
@@ -1460,9 +1476,8 @@ struct Launch {
     else if (mode == ROWS_EIGHT) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, 32 * NW), BwdQ<T, D, false, NW>::LDS, a, s);
     else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
     if (e != hipSuccess) return e;
-    if (few_keys(D, heads, a.S))
-      e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 1, 4>>(256, heads * tiles(a.S, 32) * a.row_splits, BwdKv<T, D, 1, 4>::LDS, a, s);
-    else e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 4, NW>>(64 * NW, heads * tiles(a.S, 128) * a.row_splits, BwdKv<T, D, 4, NW>::LDS, a, s);
+    if (few_keys(D, heads, a.S)) e = key_side<1, 4>(a, heads * tiles(a.S, 32) * a.row_splits, s);
+    else e = key_side<4, NW>(a, heads * tiles(a.S, 128) * a.row_splits, s);
     if (e != hipSuccess || a.row_splits == 1) return e;
     return launch<k_forms_kv_join<T>>(256, (heads * a.S * a.w / 2 + 255) / 256, 0, a, s);
   }
