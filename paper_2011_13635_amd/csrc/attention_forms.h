@@ -473,7 +473,7 @@ __device__ __forceinline__ int key_limit(const FormArgs& a, int pos, int prefix)
 struct RowOf {
   int R, qi, head, pos, id, lim;
   bool in, live;       // inside the tensor; sees anything at all
-  float slope2;
+  float slope;         // of the distance, in the scores' unit before score_factor()
 };
 __device__ __forceinline__ RowOf row_of(const FormArgs& a, int R, int b, int hk, int prefix) {
   RowOf r;
@@ -487,7 +487,7 @@ __device__ __forceinline__ RowOf row_of(const FormArgs& a, int R, int b, int hk,
   r.id = a.docs ? a.docs[(size_t)b * a.S + r.pos] : 0;
   r.live = r.in && r.id >= 0;
   r.lim = r.live ? key_limit(a, r.pos, prefix) : 0;
-  r.slope2 = a.slopes ? a.slopes[r.head] * LOG2E : 0.f;
+  r.slope = a.slopes ? a.slopes[r.head] * (a.cap > 0.f ? LOG2E : 1.f / a.scale) : 0.f;
   return r;
 }
 // Limits and document entries of the live rows among R0 .. R0 + count - 1.  Limits grow with the position: the first and the last
@@ -553,16 +553,16 @@ __device__ __forceinline__ void positions_range(const int2* r, int p0, int p1, i
 }
 
 // Scores of 32 keys from k0 on (registers) for a lane's row: cap and distance, then the mask.  What comes out times
-// score_factor() is the score in base 2; without cap and distance that leaves the factor to the exponential's own multiply-add.
-template <bool CAP, bool SLOPES>
-__device__ __forceinline__ float score_factor(const Score& f) { return CAP || SLOPES ? 1.f : f.a; }
+// score_factor() is the score in base 2; without a cap that leaves the factor to the exponential's own multiply-add.
+template <bool CAP>
+__device__ __forceinline__ float score_factor(const Score& f) { return CAP ? 1.f : f.a; }
 template <bool CAP, bool SLOPES, bool DAMP>
 __device__ __forceinline__ void open_scores(const Score& f, const RowOf& r, int k0, int half, f32x16_t& s, f32x16_t& damp) {
   if constexpr (CAP) cap_scores<DAMP>(f, s, damp);
   if constexpr (SLOPES) {
-    const float far = (float)(r.pos - k0 - 4 * half), c = CAP ? 1.f : f.a;
+    const float far = (float)(r.pos - k0 - 4 * half);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope2, fabsf(far - (float)acc_row(i)), c * s[i]);
+    for (int i = 0; i < 16; ++i) s[i] = fmaf(-r.slope, fabsf(far - (float)acc_row(i)), s[i]);
   }
 }
 // the keys that the row does not see get -infinity; limit: the least of the wavefront's rows
@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
   Frags<T, D> qf;
   load_frags<T, D>(qf, head_ptr<T>(a.q, b, r.head) + (long long)r.qi * a.q.sr, half, a.w, r.live);
   const Score sc = make_score<CAP>(a.scale, a.cap);
-  const float factor = score_factor<CAP, SLOPES>(sc);
+  const float factor = score_factor<CAP>(sc);
   const Lane<T, D> ln(lane);
   typename F::Keys kv;
   kv.init(a, b, hk, lds, tid);
@@ -925,7 +925,7 @@ template <typename T, int D, bool CAP, bool SLOPES, bool MEND, bool SPARE>
 __device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, const RowOf& r, uint32_t keys, uint32_t values, int row0, const int* ids,
                                             int k0, int limit, bool mask, const Frags<T, D>& qf, const Frags<T, D>& gf, uint32_t grad, const Lane<T, D>& ln,
                                             int half, float l2, float delta, f32x16_t (&dq)[D / 32], f32x16_t (&pk)[MEND ? D / 32 : 1], float& rest) {
-  const float factor = score_factor<CAP, SLOPES>(sc);
+  const float factor = score_factor<CAP>(sc);
   f32x16_t s = dot_rows<T, D>(keys, row0, qf, ln), dp, damp;
   if constexpr (SPARE) dp = dot_tiles<T, D>(values, row0, grad, ln);
   else dp = dot_rows<T, D>(values, row0, gf, ln);
@@ -1069,16 +1069,16 @@ __device__ __forceinline__ f32x16_t rows_of(const float* x, int half) {
 // What the key side has to know of the rows of a tile.
 template <int RT>
 struct RowsMeta {
-  float l2[RT], delta[RT], slope[RT];        // -log-sum-exp in base 2 (no cap, no slopes: over the score's factor), -delta
-  int lim[RT], id[RT], pos[RT];
-  template <bool PLAIN>
+  float l2[RT], delta[RT], slope[RT], pos[RT];      // -log-sum-exp in base 2 over score_factor(), -delta
+  int lim[RT], id[RT];
+  template <bool CAP>
   __device__ __forceinline__ void put(int i, const RowOf& r, const Score& sc, float lse, float d) {
-    l2[i] = lse == -INFINITY ? -INFINITY : -lse * (PLAIN ? LOG2E / sc.a : LOG2E);     // rows that see nothing: probabilities zero
+    l2[i] = lse == -INFINITY ? -INFINITY : -lse * (CAP ? LOG2E : LOG2E / sc.a);     // rows that see nothing: probabilities zero
     delta[i] = -d;
-    slope[i] = r.slope2;
+    slope[i] = r.slope;
     lim[i] = r.lim;
     id[i] = r.id;
-    pos[i] = r.pos;
+    pos[i] = (float)r.pos;
   }
 };
 // A wavefront's 32 keys (key: the lane's) and the rows 32 rb .. of the tiles of queries and of output gradients: dK, dV grow.
@@ -1087,8 +1087,8 @@ __device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m
                                           const Frags<T, D>& vf, uint32_t keys, uint32_t values, int key, int kid, bool mask, const Lane<T, D>& ln,
                                           int half, f32x16_t (&dk)[D / 32], f32x16_t (&dv)[D / 32]) {
   constexpr bool PLAIN = !CAP && !SLOPES;
-  // without cap and slopes the products start from what is taken off them, the row's log-sum-exp and delta
-  f32x16_t s = PLAIN ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
+  // the products start from what is taken off them, the row's log-sum-exp (no cap) and delta (no slopes either: registers)
+  f32x16_t s = !CAP ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
   if constexpr (SPARE) {
     s = dot_tiles<T, D>(queries, 32 * rb, keys, ln, s);
     dp = dot_tiles<T, D>(grads, 32 * rb, values, ln, dp);
@@ -1105,10 +1105,9 @@ __device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m
     for (int g = 0; g < 4; ++g) {
       const int at4 = 32 * rb + 8 * g + 4 * half;
       const f32x4_t sl = *reinterpret_cast<const f32x4_t*>(m.slope + at4);
-      const int4 ps = *reinterpret_cast<const int4*>(m.pos + at4);
-      const int pos[4] = {ps.x, ps.y, ps.z, ps.w};
+      const f32x4_t pos = *reinterpret_cast<const f32x4_t*>(m.pos + at4);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf((float)(pos[j] - key)), (CAP ? 1.f : sc.a) * s[4 * g + j]);
+      for (int j = 0; j < 4; ++j) s[4 * g + j] = fmaf(-sl[j], fabsf(pos[j] - (float)key), s[4 * g + j]);
     }
   }
   if (mask) {
@@ -1124,13 +1123,11 @@ __device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     f32x4_t l2 = f32x4_t{0.f, 0.f, 0.f, 0.f}, dl = l2;
-    if constexpr (!PLAIN) {
-      l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
-      dl = *reinterpret_cast<const f32x4_t*>(m.delta + 32 * rb + 8 * g + 4 * half);
-    }
+    if constexpr (CAP) l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
+    if constexpr (!PLAIN) dl = *reinterpret_cast<const f32x4_t*>(m.delta + 32 * rb + 8 * g + 4 * half);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float p = __builtin_amdgcn_exp2f(PLAIN ? sc.a * s[4 * g + j] : s[4 * g + j] + l2[j]);
+      const float p = __builtin_amdgcn_exp2f(CAP ? s[4 * g + j] + l2[j] : sc.a * s[4 * g + j]);
       s[4 * g + j] = p;
       dp[4 * g + j] = p * (PLAIN ? dp[4 * g + j] : dp[4 * g + j] + dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
     }
@@ -1161,8 +1158,7 @@ template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW, int WAVE
 __global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
   fetch_args(a);
   using K = BwdKv<T, D, BLOCKS, NW, WAVES>;
-  constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;
-  constexpr bool PLAIN = !CAP && !SLOPES;  // NR: blocks of 32 rows of a tile that a wavefront takes
+  constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;      // NR: blocks of 32 rows of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
@@ -1227,7 +1223,7 @@ __global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
   };
   auto commit = [&](int i) {
     if (tid >= RT) return;
-    meta[i & (K::BUFS - 1)].template put<PLAIN>(tid, mr, sc, ml2, mdelta);
+    meta[i & (K::BUFS - 1)].template put<CAP>(tid, mr, sc, ml2, mdelta);
   };
 
   const int all_tiles = (a.n + QT - 1) / QT, n_tiles = (all_tiles - split + a.row_splits - 1) / a.row_splits;   // every row_splits-th
@@ -1318,7 +1314,6 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
   fetch_args(a);
   static_assert(sizeof(T) == 2 && ONE * 4 <= TILE_ALIGN, "the entries' room");
   constexpr int TILE = BwdOne<T, D>::TILE;
-  constexpr bool PLAIN = !CAP && !SLOPES;
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ __attribute__((aligned(16))) RowsMeta<ONE> m;
@@ -1383,7 +1378,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
       for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
     if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
   }
-  if (half == 0) m.template put<PLAIN>(own, r, sc, lse, r.live ? delta : 0.f);
+  if (half == 0) m.template put<CAP>(own, r, sc, lse, r.live ? delta : 0.f);
 
   Frags<T, D> kf, vf;      // of the lane's key
 #pragma unroll
