@@ -288,10 +288,17 @@ __device__ __forceinline__ const int2* doc_ranges(const FormArgs& a, int b, int2
   const int blocks = (a.S + 63) / 64;
   if (!a.docs) return nullptr;
   if (most > FORM_OWN_RANGES) return a.ranges + (size_t)b * blocks;
-  for (int i = tid >> 6; i < min(most, blocks - from); i += threads >> 6) {
-    const int v = a.docs[(size_t)b * a.S + min(64 * (from + i) + (tid & 63), a.S - 1)];
-    const int lo = wave_min_i(v), hi = wave_max_i(v);
-    if ((tid & 63) == 0) room[i] = make_int2(lo, hi);
+  const int count = min(most, blocks - from), step = threads >> 6;
+  for (int i = tid >> 6; i < count; i += 4 * step) {      // four loads at a time (2x4096x8 heads of 64, documents of 128: 17 -> 14 us)
+    int v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a.docs[(size_t)b * a.S + min(64 * (from + min(i + j * step, count - 1)) + (tid & 63), a.S - 1)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i + j * step >= count) break;
+      const int lo = wave_min_i(v[j]), hi = wave_max_i(v[j]);
+      if ((tid & 63) == 0) room[i + j * step] = make_int2(lo, hi);
+    }
   }
   __syncthreads();
   return room - from;
