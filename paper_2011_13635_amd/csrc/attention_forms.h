@@ -200,6 +200,20 @@ __device__ __forceinline__ void add_outer(f32x16_t (&acc)[D / 32], uint32_t tile
       }
   }
 }
+// What rounding to bf16 took off, for a second product.  The roundings of a row's terms average out over many keys; over few, and
+// with terms that cancel, the gradient would be off by more than its own rounding.  Sequences of up to 32 keys, whose time is that of
+// a launch, take it along (1x32x4 heads of 64, backward: 7.1 -> 7.5 us; 2x4 keys, dQ: 2.5e-3 -> 1.6e-3 off, its own rounding).
+constexpr int FINE = 32;
+__device__ __forceinline__ f32x16_t lost(const f32x16_t& p) {
+  f32x16_t r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t u = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+    r[2 * i] = p[2 * i] - __uint_as_float(u << 16);
+    r[2 * i + 1] = p[2 * i + 1] - __uint_as_float(u & 0xffff0000u);
+  }
+  return r;
+}
 // two such products of the same tile (bf16)
 template <typename T, int D>
 __device__ __forceinline__ void add_outer2(f32x16_t (&x)[D / 32], f32x16_t (&y)[D / 32], uint32_t tile, int row0, const f32x16_t& p,
@@ -928,7 +942,7 @@ struct BwdQ {
   static_assert(!FEW || Keys::LDS >= 3 * 32 * D * 4 + 3 * 256, "the join's room");
 };
 // A wavefront's 32 rows and 32 keys from k0 on, row0 in the tiles of keys and values: dQ, the sums of p damp k and rest grow.
-template <typename T, int D, bool CAP, bool SLOPES, bool MEND, bool SPARE>
+template <typename T, int D, bool CAP, bool SLOPES, bool MEND, bool SPARE, bool SHORT>
 __device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, const RowOf& r, uint32_t keys, uint32_t values, int row0, const int* ids,
                                             int k0, int limit, bool mask, const Frags<T, D>& qf, const Frags<T, D>& gf, uint32_t grad, const Lane<T, D>& ln,
                                             int half, float l2, float delta, f32x16_t (&dq)[D / 32], f32x16_t (&pk)[MEND ? D / 32 : 1], float& rest) {
@@ -953,6 +967,8 @@ __device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, 
   if constexpr (MEND) {
     add_outer2<T, D>(dq, pk, keys, row0, dp, s, ln);
     feed<T, D / 16, 2, 2>();
+    if constexpr (SHORT)
+      if (a.S <= FINE) add_outer<T, D>(dq, keys, row0, lost(dp), ln);
   } else {
     add_outer<T, D>(dq, keys, row0, dp, ln);
   }
@@ -1029,7 +1045,7 @@ __global__ void __launch_bounds__(64 * NW, (BwdQ<T, D, FEW, NW>::WAVES)) k_forms
 #pragma unroll Q::SPARE ? 1 : NK
       for (int kb = 0; kb < NK; ++kb) {
         const int row0 = 32 * (FEW ? wave : kb);
-        query_block<T, D, CAP, SLOPES, MEND, Q::SPARE>(a, sc, r, kv.keys(i), kv.values(i), row0, kv.ids(i) + row0, k0 + row0, ws.lim_lo, state == 1, qf, gf,
+        query_block<T, D, CAP, SLOPES, MEND, Q::SPARE, FEW>(a, sc, r, kv.keys(i), kv.values(i), row0, kv.ids(i) + row0, k0 + row0, ws.lim_lo, state == 1, qf, gf,
                                                        lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln, half, l2, delta, dq, pk, rest);
       }
     }
@@ -1089,8 +1105,8 @@ struct RowsMeta {
   }
 };
 // A wavefront's 32 keys (key: the lane's) and the rows 32 rb .. of the tiles of queries and of output gradients: dK, dV grow.
-template <typename T, int D, bool CAP, bool SLOPES, bool SPARE, int RT>
-__device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m, uint32_t queries, uint32_t grads, int rb, const Frags<T, D>& kf,
+template <typename T, int D, bool CAP, bool SLOPES, bool SPARE, bool SHORT, int RT>
+__device__ __forceinline__ void key_block(const FormArgs& a, const Score& sc, const RowsMeta<RT>& m, uint32_t queries, uint32_t grads, int rb, const Frags<T, D>& kf,
                                           const Frags<T, D>& vf, uint32_t keys, uint32_t values, int key, int kid, bool mask, const Lane<T, D>& ln,
                                           int half, f32x16_t (&dk)[D / 32], f32x16_t (&dv)[D / 32]) {
   constexpr bool PLAIN = !CAP && !SLOPES;
@@ -1142,6 +1158,11 @@ __device__ __forceinline__ void key_block(const Score& sc, const RowsMeta<RT>& m
   add_outer<T, D>(dv, grads, 32 * rb, s, ln);
   add_outer<T, D>(dk, queries, 32 * rb, dp, ln);
   feed<T, D / 8, 2, 1>();
+  if constexpr (SHORT && sizeof(T) == 2)
+    if (a.S <= FINE) {
+      add_outer<T, D>(dv, grads, 32 * rb, lost(s), ln);
+      add_outer<T, D>(dk, queries, 32 * rb, lost(dp), ln);
+    }
 }
 
 // BLOCKS times 32 keys, over tiles of as many queries as have their rows (one for each of the G heads of the group) in RT.
@@ -1266,7 +1287,7 @@ __global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
       if (!hidden) {
 #pragma unroll 1
         for (int rb = part * NR; rb < part * NR + NR; ++rb) {
-          key_block<T, D, CAP, SLOPES, K::SPARE>(sc, m, tile, tile + TILE, rb, kf, vf, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB,
+          key_block<T, D, CAP, SLOPES, K::SPARE, BLOCKS == 1>(a, sc, m, tile, tile + TILE, rb, kf, vf, lds_addr(Ks) + blk * 32 * Tile<T, D>::ROWB,
                                                  lds_addr(Vs) + blk * 32 * Tile<T, D>::ROWB, key, kid, mask, ln, half, dk, dv);
         }
       }
@@ -1375,7 +1396,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
       positions_range(ranges, k0, k0, lo, hi);
       const int state = tile_state(a, ws, k0, 32, lo, hi);
       if (state == 0) continue;
-      query_block<T, D, CAP, SLOPES, true, false>(a, sc, r, first_tile, second_tile, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
+      query_block<T, D, CAP, SLOPES, true, false, true>(a, sc, r, first_tile, second_tile, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
     }
     rest += __shfl_xor(rest, 32, 64);
     delta += rest;
@@ -1410,7 +1431,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
     positions_range(ranges, p0, p1, lo, hi);
     if (Rw >= key_limit(a, p1, prefix) || kid_hi < 0 || (docs && (hi < kid_lo || lo > kid_hi))) continue;
     const bool mask = Rw + 32 > key_limit(a, p0, prefix) || (docs && !(lo == hi && lo == kid_lo && lo == kid_hi));
-    key_block<T, D, CAP, SLOPES, false>(sc, m, first_tile, second_tile, R0 / 32, kf, vf, 0, 0, own, kid, mask, ln, half, dk, dv);
+    key_block<T, D, CAP, SLOPES, false, true>(a, sc, m, first_tile, second_tile, R0 / 32, kf, vf, 0, 0, own, kid, mask, ln, half, dk, dv);
   }
   if (!in) return;
   store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, a.scale, live);

@@ -89,6 +89,28 @@ def test_short_sequences(shape, form):
     _case(torch, torch.bfloat16, *shape, **FORMS[form], seed=3)
 
 
+@pytest.mark.parametrize("shape", [(2, 2, 2, 2, 2, 64), (3, 4, 4, 4, 2, 128), (2, 7, 9, 2, 2, 32), (2, 32, 32, 4, 1, 64), (1, 31, 31, 2, 2, 120)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("form", [{}, {"causal": True, "cap": 10.0}, {"slopes": 0.1}])
+def test_few_keys_round_gradients_once(shape, form):
+    # Up to 32 keys the terms of a gradient go into its products in two bf16 parts.  What is left of a term is 2^-8 of what one part would
+    # lose, and so is what the stored output's rounding leaves in delta (taken out with p in one part): the bounds of those
+    # roundings times 2^-8, doubled for products of roundings, next to the gradient's own half step.
+    import torch
+    B, n, S, h, kv, w = shape
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((B, n, h, w), (B, S, kv, w), (B, S, kv, w), (B, n, h, w)))
+    slopes = torch.full((h,), form["slopes"], device="cuda") if "slopes" in form else None
+    f = {name: x for name, x in form.items() if name != "slopes"}
+    a = binding.mslt_attention(q, k, v, binding.attention_form(**f), slopes=slopes)
+    d = binding.mslt_attention_backward(q, k, v, a["out"], a["lse"], go, binding.attention_form(**f), slopes=slopes)
+    want, _ = R.attention(q, k, v, grad=go, slopes=slopes, **f)
+    for name in ("dq", "dk", "dv"):
+        value, f32, b16 = want[name]
+        own = 2.0 ** -8 * value.abs()
+        R.check(d[name], (value, f32, (b16 - own) * 2.0 ** -7 + own), True, name)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("form", [0, 5, 6])
 @pytest.mark.parametrize("shape", [(32, 128, 128, 8, 8, 64), (40, 200, 200, 8, 8, 64), (64, 256, 256, 4, 4, 128), (70, 330, 350, 8, 4, 96),
