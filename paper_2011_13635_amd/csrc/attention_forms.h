@@ -1092,11 +1092,11 @@ __device__ __forceinline__ f32x16_t rows_of(const float* x, int half) {
 // What the key side has to know of the rows of a tile.
 template <int RT>
 struct RowsMeta {
-  float l2[RT], delta[RT], slope[RT], pos[RT];      // -log-sum-exp in base 2 over score_factor(), -delta
+  float l2[RT], delta[RT], slope[RT], pos[RT];      // -log-sum-exp in base 2 (START: over score_factor()), -delta
   int lim[RT], id[RT];
-  template <bool CAP>
+  template <bool START>
   __device__ __forceinline__ void put(int i, const RowOf& r, const Score& sc, float lse, float d) {
-    l2[i] = lse == -INFINITY ? -INFINITY : -lse * (CAP ? LOG2E : LOG2E / sc.a);     // rows that see nothing: probabilities zero
+    l2[i] = lse == -INFINITY ? -INFINITY : -lse * (START ? LOG2E / sc.a : LOG2E);     // rows that see nothing: probabilities zero
     delta[i] = -d;
     slope[i] = r.slope;
     lim[i] = r.lim;
@@ -1109,9 +1109,10 @@ template <typename T, int D, bool CAP, bool SLOPES, bool SPARE, bool SHORT, int 
 __device__ __forceinline__ void key_block(const FormArgs& a, const Score& sc, const RowsMeta<RT>& m, uint32_t queries, uint32_t grads, int rb, const Frags<T, D>& kf,
                                           const Frags<T, D>& vf, uint32_t keys, uint32_t values, int key, int kid, bool mask, const Lane<T, D>& ln,
                                           int half, f32x16_t (&dk)[D / 32], f32x16_t (&dv)[D / 32]) {
-  constexpr bool PLAIN = !CAP && !SLOPES;
-  // the products start from what is taken off them, the row's log-sum-exp (no cap) and delta (no slopes either: registers)
-  f32x16_t s = !CAP ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
+  constexpr bool START = sizeof(T) == 2 && !CAP, PLAIN = START && !SLOPES;
+  // bf16: the products start from what is taken off them, the row's log-sum-exp (no cap) and delta (no slopes either: registers).
+  // fp32: not so, as every sum on the way would be rounded at that size (3x203x12 heads: dQ, dK off by 9e-7, not 5e-7).
+  f32x16_t s = START ? rows_of(m.l2 + 32 * rb, half) : zero16(), dp = PLAIN ? rows_of(m.delta + 32 * rb, half) : zero16();
   if constexpr (SPARE) {
     s = dot_tiles<T, D>(queries, 32 * rb, keys, ln, s);
     dp = dot_tiles<T, D>(grads, 32 * rb, values, ln, dp);
@@ -1146,11 +1147,11 @@ __device__ __forceinline__ void key_block(const FormArgs& a, const Score& sc, co
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     f32x4_t l2 = f32x4_t{0.f, 0.f, 0.f, 0.f}, dl = l2;
-    if constexpr (CAP) l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
+    if constexpr (!START) l2 = *reinterpret_cast<const f32x4_t*>(m.l2 + 32 * rb + 8 * g + 4 * half);
     if constexpr (!PLAIN) dl = *reinterpret_cast<const f32x4_t*>(m.delta + 32 * rb + 8 * g + 4 * half);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float p = __builtin_amdgcn_exp2f(CAP ? s[4 * g + j] + l2[j] : sc.a * s[4 * g + j]);
+      const float p = __builtin_amdgcn_exp2f(CAP ? s[4 * g + j] + l2[j] : START ? sc.a * s[4 * g + j] : fmaf(sc.a, s[4 * g + j], l2[j]));
       s[4 * g + j] = p;
       dp[4 * g + j] = p * (PLAIN ? dp[4 * g + j] : dp[4 * g + j] + dl[j]) * (CAP ? damp[4 * g + j] : 1.f);
     }
@@ -1251,7 +1252,7 @@ __global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
   };
   auto commit = [&](int i) {
     if (tid >= RT) return;
-    meta[i & (K::BUFS - 1)].template put<CAP>(tid, mr, sc, ml2, mdelta);
+    meta[i & (K::BUFS - 1)].template put<sizeof(T) == 2 && !CAP>(tid, mr, sc, ml2, mdelta);
   };
 
   const int all_tiles = (a.n + QT - 1) / QT, n_tiles = (all_tiles - split + a.row_splits - 1) / a.row_splits;   // every row_splits-th
@@ -1406,7 +1407,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
       for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
     if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
   }
-  if (half == 0) m.template put<CAP>(own, r, sc, lse, r.live ? delta : 0.f);
+  if (half == 0) m.template put<sizeof(T) == 2 && !CAP>(own, r, sc, lse, r.live ? delta : 0.f);
 
   Frags<T, D> kf, vf;      // of the lane's key
 #pragma unroll
