@@ -238,7 +238,7 @@ def _place(name, stream, first, *others):
         if t is not None and t.get_device() != index:
             raise _refusal(f"{name}: tensors on different devices")
     if stream is None and torch.cuda.current_device() == index:
-        return torch.cuda.current_stream(index).cuda_stream, None
+        return torch._C._cuda_getCurrentRawStream(index), None      # (a Stream object around it takes a microsecond)
     if stream is None:
         stream = torch.cuda.current_stream(index)
     elif stream.device.index != index:
@@ -261,15 +261,25 @@ def _precision(name, t):
 
 def _heads(name, what, t, like=None, shape=None):
     """A 4-D tensor [batch, rows, heads, width] as the C struct; like: must have its type."""
-    if t.dim() != 4 or (shape is not None and t.shape != shape):
+    st, got = t.stride(), t.shape
+    if len(st) != 4 or (shape is not None and got != shape):
         raise _refusal(f"{name}: {what} must be [batch, rows, heads, width]" + (f" {tuple(shape)}" if shape is not None else "") +
-                       f", not {tuple(t.shape)}")
+                       f", not {tuple(got)}")
     if like is not None and t.dtype is not like.dtype:
         raise _refusal(f"{name}: {what} is {t.dtype}, not {like.dtype}")
-    sb, sr, sh, se = t.stride()
-    if se != 1 and t.shape[3] > 1:
+    if st[3] != 1 and got[3] > 1:
         raise _refusal(f"{name}: the elements of a head of {what} must be next to each other")
-    return Heads(t.data_ptr(), sb, sr, sh)
+    return Heads(t.data_ptr(), st[0], st[1], st[2])
+
+
+def _result(name, what, given, like):
+    """The tensor a result goes to and its C struct: the given one, or a new contiguous one of like's shape and type."""
+    import torch
+    if given is not None:
+        return given, _heads(name, what, given, like, like.shape)
+    t = torch.empty_like(like, memory_format=torch.contiguous_format)
+    _, S, h, w = like.shape
+    return t, Heads(t.data_ptr(), S * h * w, h * w, w)
 
 
 def _flat(name, what, t, dtype, *shapes):
@@ -294,16 +304,15 @@ def rotary_form(rotary_width, interleaved=False, theta=10000.0, scaling="none", 
 
 
 def _rotary_sizes(name, q, k):
-    B, S, hq, w = q.shape if q.dim() == 4 else (0, 0, 0, 0)
-    if k is not None and (k.dim() != 4 or (k.shape[0], k.shape[1], k.shape[3]) != (B, S, w)):
+    if q.dim() != 4:
+        return 0, 0, 0, 0, 0      # (the operand itself is refused where its struct is made)
+    B, S, hq, w = q.shape
+    if k is None:
+        return B, S, hq, 0, w
+    kb, ks, hk, kw = k.shape if k.dim() == 4 else (0, 0, 0, 0)
+    if kb != B or ks != S or kw != w:
         raise _refusal(f"{name}: q {tuple(q.shape)} and k {tuple(k.shape)} differ in more than their heads")
-    return B, S, hq, 0 if k is None else k.shape[2], w
-
-
-def _result(given, like):
-    """The tensor a result goes to: the given one, or a new contiguous one."""
-    import torch
-    return given if given is not None else torch.empty_like(like, memory_format=torch.contiguous_format)
+    return B, S, hq, hk, w
 
 
 def _given(name, what, given, n):
@@ -326,14 +335,15 @@ def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None,
         with place:
             return mslt_rotary(q, k, form, positions, inverse, out)
     B, S, hq, hk, w = _rotary_sizes(name, q, k)
-    oq = _result(oq, q)
-    kin = kout = None
+    qin, kin, kout = _heads(name, "q", q), None, None
+    oq, qout = _result(name, "out", oq, q)
     if k is not None:
-        ok = _result(ok, k)
-        kin, kout = C.byref(_heads(name, "k", k, q)), C.byref(_heads(name, "out", ok, q, k.shape))
-    _check(load_library().mslt_rotary(st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), kin,
+        kin = C.byref(_heads(name, "k", k, q))
+        ok, kout = _result(name, "out", ok, k)
+        kout = C.byref(kout)
+    _check(load_library().mslt_rotary(st, _precision(name, q), B, S, hq, hk, w, C.byref(qin), kin,
                                       _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form), int(inverse),
-                                      C.byref(_heads(name, "out", oq, q, q.shape)), kout))
+                                      C.byref(qout), kout))
     return oq, ok
 
 
@@ -355,11 +365,12 @@ def mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form: RotaryForm, positions
         with place:
             return mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form, positions, out)
     B, S, hq, hk, w = _rotary_sizes(name, q, k)
-    oq, ok = _result(oq, q), _result(ok, k)
+    qin, kin = _heads(name, "q", q), _heads(name, "k", k, q)
+    (oq, qout), (ok, kout) = _result(name, "out", oq, q), _result(name, "out", ok, k)
     _check(load_library().mslt_head_norm_rotary(
-        st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)),
+        st, _precision(name, q), B, S, hq, hk, w, C.byref(qin), C.byref(kin),
         *_gains(name, gain_q, gain_k, hq, hk, w), eps, _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
-        C.byref(_heads(name, "out", oq, q, q.shape)), C.byref(_heads(name, "out", ok, q, k.shape))))
+        C.byref(qout), C.byref(kout)))
     return oq, ok
 
 
@@ -375,17 +386,17 @@ def mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form: RotaryForm, 
             return mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form, grad_q, grad_k, positions, out)
     B, S, hq, hk, w = _rotary_sizes(name, q, k)
     gains = _gains(name, gain_q, gain_k, hq, hk, w)
-    dq, dk = _result(dq, q), _result(dk, k)
+    qin, kin = _heads(name, "q", q), _heads(name, "k", k, q)
+    (dq, qout), (dk, kout) = _result(name, "out", dq, q), _result(name, "out", dk, k)
     dgq, dgk = torch.empty_like(gain_q), torch.empty_like(gain_k)
     need = C.c_size_t()
     _check(lib.mslt_head_norm_workspace(B, S, hq, hk, w, C.byref(need)))
     ws = gain_q.new_empty(need.value // 4 + 1)
     _check(lib.mslt_head_norm_rotary_backward(
-        st, _precision(name, q), B, S, hq, hk, w, C.byref(_heads(name, "q", q)), C.byref(_heads(name, "k", k, q)), *gains, eps,
+        st, _precision(name, q), B, S, hq, hk, w, C.byref(qin), C.byref(kin), *gains, eps,
         _flat(name, "positions", positions, torch.int32, (B, S)), C.byref(form),
         C.byref(_heads(name, "grad_q", grad_q, q, q.shape)), C.byref(_heads(name, "grad_k", grad_k, q, k.shape)),
-        C.byref(_heads(name, "out", dq, q, q.shape)), C.byref(_heads(name, "out", dk, q, k.shape)),
-        dgq.data_ptr(), dgk.data_ptr(), ws.data_ptr(), need.value))
+        C.byref(qout), C.byref(kout), dgq.data_ptr(), dgk.data_ptr(), ws.data_ptr(), need.value))
     return {"dq": dq, "dk": dk, "dgain_q": dgq, "dgain_k": dgk}
 
 
@@ -425,11 +436,10 @@ def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, sl
         with place:
             return mslt_attention(q, k, v, form, documents, prefix, slopes, out)
     sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
-    out = _result(out, q)
+    out, o = _result(name, "out", out, q)
     lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32)
     ws, room = _attention_workspace(lib, sizes, 0, lse)
-    _check(lib.mslt_attention(st, *sizes, *qkv, C.byref(f), C.byref(_heads(name, "out", out, q, q.shape)), lse.data_ptr(),
-                              ws.data_ptr(), room))
+    _check(lib.mslt_attention(st, *sizes, *qkv, C.byref(f), C.byref(o), lse.data_ptr(), ws.data_ptr(), room))
     return {"out": out, "lse": lse}
 
 
@@ -445,13 +455,13 @@ def mslt_attention_backward(q, k, v, out, lse, grad_out, form: AttentionForm, do
         with place:
             return mslt_attention_backward(q, k, v, out, lse, grad_out, form, documents, prefix, slopes, grads)
     sizes, qkv, f = _attention_call(name, q, k, v, form, documents, prefix, slopes)
-    dq, dk, dv = _result(dq, q), _result(dk, k), _result(dv, v)
+    (dq, q_out), (dk, k_out), (dv, v_out) = _result(name, "grads", dq, q), _result(name, "grads", dk, k), _result(name, "grads", dv, k)
     ws, room = _attention_workspace(lib, sizes, 1, lse)
     _check(lib.mslt_attention_backward(
         st, *sizes, *qkv, C.byref(_heads(name, "out", out, q, q.shape)),
         _flat(name, "lse", lse, torch.float32, (q.shape[0], q.shape[2], q.shape[1])),
-        C.byref(_heads(name, "grad_out", grad_out, q, q.shape)), C.byref(f), C.byref(_heads(name, "grads", dq, q, q.shape)),
-        C.byref(_heads(name, "grads", dk, q, k.shape)), C.byref(_heads(name, "grads", dv, q, k.shape)), ws.data_ptr(), room))
+        C.byref(_heads(name, "grad_out", grad_out, q, q.shape)), C.byref(f), C.byref(q_out), C.byref(k_out), C.byref(v_out),
+        ws.data_ptr(), room))
     return {"dq": dq, "dk": dk, "dv": dv}
 
 
