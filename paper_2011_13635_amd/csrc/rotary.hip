@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(256) k_head_sums(RotaryArgs a) {
 // head, 2^lg lanes a head; a workgroup takes `group` heads of `abreast` tokens at a time and U such sets in a row, all their
 // loads issued first.  Sine and cosine of the tokens are worked out once for all heads, in LDS.  A lane keeps its head and
 // piece, so gains and their gradients stay in registers.  Bound by memory: 4x16384 tokens of 16+4 heads of 128, 671 MB, 129 us,
-// 5.2 TB/s (a large copy 4.7); with norm and gradients 32x512 tokens of 16+16 heads of 64, 336 MB, 87 us.  One wavefront per
+// 5.2 TB/s (a large copy 4.7); with norm and gradients 32x512 tokens of 16+16 heads of 64, 336 MB, 76 us.  One wavefront per
 // head (k_rotary_any) takes 628 and 998 us for the same, its sines and cosines worked out by every head.
 template <typename T>
 struct Piece {
@@ -159,7 +159,10 @@ __device__ __forceinline__ float row_sum(float v, int lg) {
   return v;
 }
 
-constexpr int U = 4, MAX_THREADS = 512;
+constexpr int MAX_THREADS = 512;
+// Sets of tokens whose loads go out together.  With the norm, whose gradient reads two tensors, registers for more wavefronts are worth
+// more than more loads of each (32x512 tokens of 16+16 heads of 64, forward and backward: four sets 85 us, two 76, one 78).
+constexpr int sets_ahead(bool norm) { return norm ? 2 : 4; }
 struct RowsPlan {
   int lg, group, abreast, groups, threads, slices;   // grid: slices x groups
   int flat;                                          // tokens lie at one stride across sequences
@@ -167,7 +170,7 @@ struct RowsPlan {
 
 template <typename T, bool NORM, bool BWD, bool INTER>
 __global__ void __launch_bounds__(MAX_THREADS) k_rotary_rows(RotaryArgs a, RowsPlan pl) {
-  constexpr int CH = Piece<T>::CH;
+  constexpr int CH = Piece<T>::CH, U = sets_ahead(NORM);
   extern __shared__ __attribute__((aligned(16))) float lds[];
   const int tid = threadIdx.x, lane = tid & 63, c = tid & ((1 << pl.lg) - 1), slot = tid >> pl.lg, heads = a.hq + a.hk;
   const int sub = slot / pl.group, h = blockIdx.y * pl.group + slot % pl.group;
@@ -334,8 +337,8 @@ bool whole_pieces(const FormHeads& x, const RotaryArgs& a, int heads, int esize)
 bool one_stride(const FormHeads& x, const RotaryArgs& a) { return !x.p || a.B == 1 || x.sb == a.S * x.sr; }
 
 // Workgroups a chip of 256 compute units keeps busy; a slice of tokens beyond that is a turn of the loop.  With gradients of the
-// gains fewer, as each leaves a row of partial sums.
-int most_slices(bool partial) { return partial ? 512 : 4096; }
+// gains fewer, three to a unit, as each leaves a row of partial sums (the same case: 512 workgroups 82 us, 768 76, 1280 82).
+int most_slices(bool partial) { return partial ? 768 : 4096; }
 RowsPlan plan_rows(const RotaryArgs& a, int esize, bool partial) {
   RowsPlan p{};
   const int pieces = a.w * esize / 16, heads = a.hq + a.hk;
@@ -348,7 +351,8 @@ RowsPlan plan_rows(const RotaryArgs& a, int esize, bool partial) {
   if (p.abreast < 1) p.abreast = 1;
   while (p.abreast > 1 && (long long)p.abreast > tokens) --p.abreast;
   p.threads = ((p.group * p.abreast << p.lg) + 63) / 64 * 64;
-  const long long sets = (tokens + U * p.abreast - 1) / (U * p.abreast);
+  const int ahead = sets_ahead(a.gain_q != nullptr);
+  const long long sets = (tokens + ahead * p.abreast - 1) / (ahead * p.abreast);
   const int limit = most_slices(partial) / p.groups > 1 ? most_slices(partial) / p.groups : 1;
   p.slices = (int)(sets < limit ? sets : limit);
   p.flat = one_stride(a.q, a) && one_stride(a.k, a) && one_stride(a.gq, a) && one_stride(a.gk, a) && one_stride(a.oq, a) && one_stride(a.ok, a);
@@ -358,7 +362,7 @@ int token_slices(long long tokens) { return (int)(tokens < 512 ? tokens : 512); 
 
 template <typename T, bool NORM, bool BWD>
 hipError_t rows_t(const RotaryArgs& a, const RowsPlan& p, hipStream_t s) {
-  const int trig = 2 * U * p.abreast * a.pairs, sums = NORM && BWD ? p.group * p.abreast * a.w : 0;
+  const int trig = 2 * sets_ahead(NORM) * p.abreast * a.pairs, sums = NORM && BWD ? p.group * p.abreast * a.w : 0;
   const int lds = (trig > sums ? trig : sums) * (int)sizeof(float);
   const dim3 grid((unsigned)p.slices, (unsigned)p.groups), block((unsigned)p.threads);
   if (a.interleaved) k_rotary_rows<T, NORM, BWD, true><<<grid, block, lds, s>>>(a, p);
@@ -401,8 +405,9 @@ hipError_t run_t(const RotaryArgs& a, bool backward, hipStream_t s) {
 
 size_t rotary_partial_floats(long long tokens, int heads, int w) {
   // every kernel's rows: per head and slice, behind them two widths a slice, or two widths for each of the slices and groups
-  const size_t any = (size_t)token_slices(tokens) * (heads + 2) * w, rows = (size_t)(most_slices(true) + heads) * 2 * w;
-  return any > rows ? any : rows;
+  const size_t slices = (size_t)(tokens < most_slices(true) ? tokens : most_slices(true));
+  const size_t any = (size_t)token_slices(tokens) * (heads + 2) * w, each = slices * heads * w, rows = (size_t)(most_slices(true) + heads) * 2 * w;
+  return any > each ? (any > rows ? any : rows) : (each > rows ? each : rows);
 }
 hipError_t rotary_run(int dtype, const RotaryArgs& a, bool backward, hipStream_t s) {
   return dtype ? run_t<bf16>(a, backward, s) : run_t<float>(a, backward, s);
