@@ -222,6 +222,36 @@ def test_layouts(dtype):
     assert (packed[:, S:] == 7).all() and (out2[:, :, S:] == 7).all()        # rows behind the last one stay as they were
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(2, 140, 140, 4, 2, 64), (2, 3, 140, 4, 2, 128), (2, 90, 90, 4, 2, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_offsets_beyond_32_bits(shape, dtype):
+    """Rows as far apart as they may be, heads and sequences 2^31 and 2^32 elements apart."""
+    import torch
+    dt = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    B, n, S, h, kv, w = shape
+    far = (1 << 32, 1 << 22, 1 << 31)
+    room = torch.empty((1 << 32) + (1 << 31) + S * (1 << 22), dtype=dt, device="cuda")
+
+    def spread(x, at, strides):
+        y = room.as_strided(x.shape, (*strides, 1), at)
+        y.copy_(x)
+        return y
+
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda").to(dt) for s in ((B, n, h, w), (B, S, kv, w), (B, S, kv, w), (B, n, h, w)))
+    form = binding.attention_form(cap=15.0, causal=True)
+    f = binding.mslt_attention(q, k, v, form)
+    d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form)
+    near = (1 << 32, 1 << 22, 1 << 12)
+    q2, go2 = spread(q, 1024, near), spread(go, 1 << 20, near)
+    k2, v2 = spread(k, 0, far), spread(v, 256, far)
+    grads = tuple(room.as_strided(x.shape, (*far, 1), at) for x, at in ((k, 512), (v, 768)))
+    f2 = binding.mslt_attention(q2, k2, v2, form)
+    d2 = binding.mslt_attention_backward(q2, k2, v2, f2["out"], f2["lse"], go2, form, grads=(torch.empty_like(q), *grads))
+    for name, want in {**f, **d}.items():
+        assert torch.equal({**f2, **d2}[name], want), name
+
+
 @pytest.mark.parametrize("n", [1, 90])
 def test_same_values_every_time_on_any_stream_and_in_graphs(n):
     import torch

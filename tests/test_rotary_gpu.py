@@ -138,6 +138,29 @@ def test_layouts(dtype):
     assert (room == 5).all()
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_offsets_beyond_32_bits(dtype):
+    import torch
+    dt = getattr(torch, dtype)
+    B, S, hq, hk, w = 2, 21, 4, 2, 64
+    q, k, rand = _inputs(torch, dt, B, S, hq, hk, w, 2)
+    f = binding.rotary_form(64)
+    room = torch.empty((1 << 32) + 4 * (1 << 30) + S * (1 << 20), dtype=dt, device="cuda")
+
+    def spread(x, at):
+        y = room.as_strided(x.shape, (1 << 32, 1 << 20, 1 << 30, 1), at)
+        y.copy_(x)
+        return y
+
+    gains = [1 + 0.3 * rand(w) for _ in range(2)]
+    q2, k2 = spread(q, 0), spread(k, 64)
+    for got, want in zip(binding.mslt_rotary(q2, k2, f), binding.mslt_rotary(q, k, f)):
+        assert torch.equal(got, want)
+    a, b = (binding.mslt_head_norm_rotary_backward(*x, *gains, 1e-6, f, *x) for x in ((q, k), (q2, k2)))
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+
+
 def test_padding_rows_of_zeros_and_large_values():
     import torch
     x = torch.zeros(1, 3, 2, 64, device="cuda")
