@@ -490,6 +490,10 @@ __device__ __forceinline__ int key_limit(const FormArgs& a, int pos, int prefix)
   return a.causal ? min(a.S, max(pos + 1, prefix)) : a.S;
 }
 
+// Factor of the gradients of queries and keys.  The softmax of a single score is one whatever the score: they are zero, where the
+// roundings of dp and delta would leave something.
+__device__ __forceinline__ float score_gradient(const FormArgs& a) { return a.S > 1 ? a.scale : 0.f; }
+
 // What a lane that owns a query row knows of it.
 struct RowOf {
   int R, qi, head, pos, id, lim;
@@ -1073,7 +1077,7 @@ __global__ void __launch_bounds__(64 * NW, (BwdQ<T, D, FEW, NW>::WAVES)) k_forms
   }
   if (!r.in) return;
   if (half == 0) a.delta[lrow] = delta;
-  store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
+  store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, score_gradient(a), r.live);
 }
 
 // the 16 of 32 rows' values that this half-wave's registers stand for
@@ -1304,10 +1308,10 @@ __global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
   if (a.row_splits > 1) {
     const size_t all = (size_t)a.B * a.nkv * a.S, row = ((size_t)b * a.nkv + hk) * a.S + key;
     float* const out = a.part + ((size_t)split * 2 * all + row) * a.w;
-    store_row<float, D>(out, dk, half, a.w, a.scale, live);
+    store_row<float, D>(out, dk, half, a.w, score_gradient(a), live);
     store_row<float, D>(out + all * a.w, dv, half, a.w, 1.f, live);
   } else {
-    store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, a.scale, live);
+    store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, score_gradient(a), live);
     store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)key * a.dv.sr, dv, half, a.w, 1.f, live);
   }
 }
@@ -1405,7 +1409,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
-    if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, a.scale, r.live);
+    if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, score_gradient(a), r.live);
   }
   if (half == 0) m.template put<sizeof(T) == 2 && !CAP>(own, r, sc, lse, r.live ? delta : 0.f);
 
@@ -1435,7 +1439,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
     key_block<T, D, CAP, SLOPES, false, true>(a, sc, m, first_tile, second_tile, R0 / 32, kf, vf, 0, 0, own, kid, mask, ln, half, dk, dv);
   }
   if (!in) return;
-  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, a.scale, live);
+  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, score_gradient(a), live);
   store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)own * a.dv.sr, dv, half, a.w, 1.f, live);
 }
 

@@ -89,6 +89,22 @@ def test_short_sequences(shape, form):
     _case(torch, torch.bfloat16, *shape, **FORMS[form], seed=3)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("w", [32, 128])
+def test_one_key_has_no_score_gradient(w, dtype):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v, go = (torch.randn((3, 1, heads, w), generator=g, device="cuda").to(getattr(torch, dtype)) for heads in (4, 2, 2, 4))
+    for form in (binding.attention_form(), binding.attention_form(cap=20.0, causal=True)):
+        f = binding.mslt_attention(q, k, v, form)
+        d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form)
+        assert (d["dq"] == 0).all() and (d["dk"] == 0).all()
+        # (out is p v / p, p being 2 to what rounding the maximum took off: off v by the roundings of the product and the quotient)
+        want, _ = R.attention(q, k, v, cap=form.cap, causal=bool(form.causal), grad=go)
+        for name in ("out", "dv"):
+            R.check({**f, **d}[name], want[name], dtype == "bfloat16", name)
+
+
 @pytest.mark.parametrize("shape", [(2, 2, 2, 2, 2, 64), (3, 4, 4, 4, 2, 128), (2, 7, 9, 2, 2, 32), (2, 32, 32, 4, 1, 64), (1, 31, 31, 2, 2, 120)],
                          ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("form", [{}, {"causal": True, "cap": 10.0}, {"slopes": 0.1}])
