@@ -190,14 +190,29 @@ __device__ __forceinline__ void add_outer(f32x16_t (&acc)[D / 32], uint32_t tile
     const bf16x8_t f[2] = {pack_frag(p, 0), pack_frag(p, 1)};
     add_packed<D>(acc, tile, row0, f, l);
   } else {
+    // The reads of the next two rows are on their way while those at hand are multiplied; left to itself the compiler waits for each
+    // read in turn (4x1024x8 heads of 64: forward 96 -> 88 us, backward 322 -> 292).
     const uint32_t at = tile + l.cols;
+    float x[2][2][D / 32];
+    auto read = [&](int g) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        const float x = lds_read<float>((at ^ (16 * (8 * db + (r & 3) + ((r >> 2) & 1) * 4))) + (row0 + acc_row(r)) * Tile<T, D>::ROWB);
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[r], acc[db], 0, 0, 0);
-      }
+        for (int db = 0; db < D / 32; ++db) {
+          const int r = 2 * g + i;
+          x[g & 1][i][db] = lds_read<float>((at ^ (16 * (8 * db + (r & 3) + ((r >> 2) & 1) * 4))) + (row0 + acc_row(r)) * Tile<T, D>::ROWB);
+        }
+    };
+    read(0);
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      if (g + 1 < 8) read(g + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[g & 1][i][db], p[2 * g + i], acc[db], 0, 0, 0);
+    }
   }
 }
 // What rounding to bf16 took off, for a second product.  The roundings of a row's terms average out over many keys; over few, and
@@ -1175,22 +1190,21 @@ __device__ __forceinline__ void key_block(const FormArgs& a, const Score& sc, co
 //   4 of 4: 128 keys, tiles of 64 rows.  4 of 8 (bf16 at width 128): the same, two wavefronts to 32 keys; keys and values stay in
 //   LDS, as the accumulators fill the registers.  1 of 4 (few keys in all): 32 keys, tiles of 128 rows.
 // Few workgroups: the rows are split over a.row_splits workgroups, whose sums k_forms_kv_join adds.
-// Wavefronts that share a SIMD: two at width 64, and of a workgroup of eight.  fp32 at width 64: two cost spilled registers, and the
-// second stage of the tiles, and pay only where there are workgroups for them (4x1024x8 heads, both sides: 369 us with one, 322 with
-// two; 1x512x12 heads, 192 workgroups: 60 and 65).
-template <typename T, int D, int BLOCKS, int NW, int WAVES>
+template <typename T, int D, int BLOCKS, int NW>
 struct BwdKv {
   static constexpr int PARTS = NW / BLOCKS, RT = PARTS == 4 ? 128 : 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
-  static constexpr int BUFS = TILE > (NW == 4 && WAVES == 2 ? 32767 : 32768) ? 1 : 2;
+  // Wavefronts that share a SIMD (fp32 at width 64 spills a few registers for it and has one stage: 4x1024x8 heads, both sides, 369 us
+  // with one, 322 with two; 3x203x12, a workgroup to each compute unit, 36 and 37).
+  static constexpr int WAVES = D == 64 || NW == 8 ? 2 : 1, BUFS = TILE > (NW == 4 && WAVES == 2 ? 32767 : 32768) ? 1 : 2;
   static constexpr bool SPARE = NW == 8;
   static constexpr int LDS = BUFS * STAGE + (SPARE ? 2 * 128 * Tile<T, D>::ROWB : 0);
   using Meta = RowsMeta<RT>;
   static_assert(BUFS * STAGE >= (PARTS - 1) * BLOCKS * 32 * D * 4, "the sums' room");
 };
-template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW, int WAVES>
-__global__ void __launch_bounds__(64 * NW, WAVES) k_forms_bwd_kv(FormArgs a) {
+template <typename T, int D, bool CAP, bool SLOPES, int BLOCKS, int NW>
+__global__ void __launch_bounds__(64 * NW, (BwdKv<T, D, BLOCKS, NW>::WAVES)) k_forms_bwd_kv(FormArgs a) {
   fetch_args(a);
-  using K = BwdKv<T, D, BLOCKS, NW, WAVES>;
+  using K = BwdKv<T, D, BLOCKS, NW>;
   constexpr int RT = K::RT, TILE = K::TILE, NR = RT / 32 / K::PARTS, KEYS = 32 * BLOCKS;      // NR: blocks of 32 rows of a tile that a wavefront takes
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ TileList list;
@@ -1483,16 +1497,6 @@ struct Launch {
     if (e != hipSuccess || a.splits == 1) return e;
     return launch<k_forms_join<T>>(256, (heads * rows + 3) / 4, 0, a, s);
   }
-  template <int BLOCKS, int WAVEFRONTS, int WAVES>
-  static hipError_t key_side_of(const FormArgs& a, size_t blocks, hipStream_t s) {
-    return launch<k_forms_bwd_kv<T, D, CAP, SLOPES, BLOCKS, WAVEFRONTS, WAVES>>(64 * WAVEFRONTS, blocks, BwdKv<T, D, BLOCKS, WAVEFRONTS, WAVES>::LDS, a, s);
-  }
-  template <int BLOCKS, int WAVEFRONTS>
-  static hipError_t key_side(const FormArgs& a, size_t blocks, hipStream_t s) {
-    if constexpr (sizeof(T) == 4 && D == 64 && BLOCKS == 1)
-      if (blocks <= 256) return key_side_of<BLOCKS, WAVEFRONTS, 1>(a, blocks, s);
-    return key_side_of<BLOCKS, WAVEFRONTS, D == 64 || WAVEFRONTS == 8 ? 2 : 1>(a, blocks, s);
-  }
   static hipError_t bwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv;
@@ -1504,8 +1508,9 @@ struct Launch {
     else if (mode == ROWS_EIGHT) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, 32 * NW), BwdQ<T, D, false, NW>::LDS, a, s);
     else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
     if (e != hipSuccess) return e;
-    if (few_keys(D, heads, a.S)) e = key_side<1, 4>(a, heads * tiles(a.S, 32) * a.row_splits, s);
-    else e = key_side<4, NW>(a, heads * tiles(a.S, 128) * a.row_splits, s);
+    if (few_keys(D, heads, a.S))
+      e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 1, 4>>(256, heads * tiles(a.S, 32) * a.row_splits, BwdKv<T, D, 1, 4>::LDS, a, s);
+    else e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 4, NW>>(64 * NW, heads * tiles(a.S, 128) * a.row_splits, BwdKv<T, D, 4, NW>::LDS, a, s);
     if (e != hipSuccess || a.row_splits == 1) return e;
     return launch<k_forms_kv_join<T>>(256, (heads * a.S * a.w / 2 + 255) / 256, 0, a, s);
   }
