@@ -408,8 +408,8 @@ __device__ __forceinline__ void load_frags(Frags<T, D>& f, const T* row, int hal
 // lane fetches is free, which is where the swizzle lives.  A lane whose piece is none of the operand's (a row past the end, a
 // row of padding, elements past the width) fetches beyond the buffer's end, which writes zeros.
 // The load is written out: behind the builtin the compiler lets every transposed read wait for all loads on their way, as it
-// cannot tell the tiles apart (1x8192, 16 heads of 128, backward: queries 801 us, 689 written out; keys 1090, 924).  It returns nothing to a register; wait_loads()
-// and a barrier stand between it and the reads.
+// cannot tell the tiles apart (1x8192, 16 heads of 128, backward: queries 801 us, 689 written out; keys 1090, 924).  It returns
+// nothing to a register; landed() stands between it and the reads.
 constexpr uint32_t NOWHERE = 0x80000000u;
 struct Source {
   u32x4_t rsrc;
@@ -455,15 +455,6 @@ struct Loader {
     }
   }
 };
-// At most `later` stages of PER loads of this wavefront are still on their way.
-template <int PER, int STAGES>
-__device__ __forceinline__ void wait_loads(int later) {
-  static_assert(STAGES <= 4 && (STAGES - 2) * PER < 64, "the counter's range");
-  constexpr auto vmcnt = [](int n) { return 0x0F70 | (n & 15) | ((n >> 4) << 14); };
-  if (STAGES > 3 && later >= 2) __builtin_amdgcn_s_waitcnt(vmcnt(2 * PER));
-  else if (STAGES > 2 && later >= 1) __builtin_amdgcn_s_waitcnt(vmcnt(PER));
-  else __builtin_amdgcn_s_waitcnt(vmcnt(0));
-}
 __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
@@ -471,10 +462,9 @@ __device__ __forceinline__ void meet() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("" ::: "memory");
 }
-// The loads of the stage at hand have landed, this wavefront's and then every one's.
-template <int PER, int STAGES>
-__device__ __forceinline__ void landed(int later) {
-  wait_loads<PER, STAGES>(later);
+// The loads on their way have landed, this wavefront's and then every one's.
+__device__ __forceinline__ void landed() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
   meet();
 }
 
@@ -635,7 +625,6 @@ struct KeyTiles {
   static constexpr int TILE = KT * Tile<T, D>::ROWB, IDS = 512, STAGE = 2 * TILE + IDS, LDS = STAGES * STAGE;
   static_assert(KT * 4 <= IDS && TILE % TILE_ALIGN == 0, "tiles start on whole rows");
   using Load = Loader<T, D, KT, NW>;
-  static constexpr int PER = 2 * Load::NI;      // loads of a wavefront for a stage (a wavefront with entries of documents: one more)
   Load kl, vl;
   const T *k, *v;
   const int32_t* docs;
@@ -671,12 +660,12 @@ struct KeyTiles {
   }
   __device__ __forceinline__ void next(int i, const TileList& list, int count, int tid) const {
     if constexpr (STAGES > 1) {
-      landed<PER, STAGES>(count - 1 - i);
+      landed();
       if (i + STAGES - 1 < count) issue(i + STAGES - 1, list, tid);
     } else {
       __syncthreads();
       issue(i, list, tid);
-      landed<PER, 1>(0);
+      landed();
     }
   }
 };
@@ -1297,7 +1286,7 @@ __global__ void __launch_bounds__(64 * NW, (BwdKv<T, D, BLOCKS, NW>::WAVES)) k_f
         commit(i);
       }
       __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): what commit() wrote
-      landed<0, 2>(0);
+      landed();
       if (K::BUFS > 1 && i + 1 < count) fetch(i + 1);
       const typename K::Meta& m = meta[i & (K::BUFS - 1)];
       const uint32_t tile = lds_addr(tiles(i));
@@ -1400,7 +1389,7 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
   const Lane<T, D> ln(lane);
   float delta = 0.f, rest = 0.f;
   __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): the entries
-  landed<0, 2>(0);
+  landed();
 #pragma unroll
   for (int s = 0; s < Tile<T, D>::NS; ++s) delta += dot_chunk<T>(gf[s], of[s]);
   delta += __shfl_xor(delta, 32, 64);
