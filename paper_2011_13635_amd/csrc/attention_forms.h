@@ -1340,16 +1340,23 @@ __global__ void __launch_bounds__(256) k_forms_kv_join(FormArgs a) {
 // registers into the tiles of the keys and values, whose own go into registers.
 // 64x128x16 heads of 64, 134 MB: 52 us against 67 of the two kernels.  Its loads and stores alone take 33, each side's products 10
 // more: the registers hold two wavefronts a SIMD, too few for loads and products to overlap.  Three, of 168 registers, spill: 54.
+// At width 128 and in fp32 the registers hold one: 64x128x8 heads of 128 80 -> 69 us, 16x128x8 52 -> 31, 128x20x16 194 -> 138.
 constexpr int ONE = 128;
 template <typename T, int D>
 struct BwdOne {
   static constexpr int TILE = ONE * Tile<T, D>::ROWB, LDS = 2 * TILE + TILE_ALIGN;
+  static constexpr int WAVES = sizeof(T) == 2 && D == 64 ? 2 : 1;      // that share a SIMD: registers
+  static constexpr bool MEND = sizeof(T) == 2;
+  // Keys and rows up to which it is taken.  fp32: four blocks of 32 one behind the other take longer than on four wavefronts (1x128x8
+  // heads of 64: 43 us against 26, 16x128x8 45 and 39; but 56x54x8 50 and 74, 1x20x4 16 and 26).
+  static constexpr int MOST = sizeof(T) == 2 ? ONE : 64;
 };
 template <typename T, int D, bool CAP, bool SLOPES>
-__global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
+__global__ void __launch_bounds__(256, (BwdOne<T, D>::WAVES)) k_forms_bwd_one(FormArgs a) {
   fetch_args(a);
-  static_assert(sizeof(T) == 2 && ONE * 4 <= TILE_ALIGN, "the entries' room");
+  static_assert(ONE * 4 <= TILE_ALIGN, "the entries' room");
   constexpr int TILE = BwdOne<T, D>::TILE;
+  constexpr bool MEND = BwdOne<T, D>::MEND;
   extern __shared__ __attribute__((aligned(TILE_ALIGN))) unsigned char lds[];
   __shared__ int2 ranges_s[FORM_OWN_RANGES];
   __shared__ __attribute__((aligned(16))) RowsMeta<ONE> m;
@@ -1395,23 +1402,27 @@ __global__ void __launch_bounds__(256, 2) k_forms_bwd_one(FormArgs a) {
   delta += __shfl_xor(delta, 32, 64);
 
   {
-    f32x16_t dq[D / 32], pk[D / 32];
+    f32x16_t dq[D / 32], pk[MEND ? D / 32 : 1];
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) dq[i] = pk[i] = zero16();
+    for (int i = 0; i < D / 32; ++i) dq[i] = zero16();
+#pragma unroll
+    for (int i = 0; MEND && i < D / 32; ++i) pk[i] = zero16();
 #pragma unroll 1
     for (int k0 = 0; k0 < a.S; k0 += 32) {
       int lo, hi;
       positions_range(ranges, k0, k0, lo, hi);
       const int state = tile_state(a, ws, k0, 32, lo, hi);
       if (state == 0) continue;
-      query_block<T, D, CAP, SLOPES, true, false, true>(a, sc, r, first_tile, second_tile, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
+      query_block<T, D, CAP, SLOPES, MEND, false, true>(a, sc, r, first_tile, second_tile, k0, ids + k0, k0, ws.lim_lo, state == 1, qf, gf, 0, ln, half, l2, delta, dq, pk, rest);
     }
-    rest += __shfl_xor(rest, 32, 64);
-    delta += rest;
+    if constexpr (MEND) {
+      rest += __shfl_xor(rest, 32, 64);
+      delta += rest;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+      for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
+        for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
+    }
     if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, score_gradient(a), r.live);
   }
   if (half == 0) m.template put<sizeof(T) == 2 && !CAP>(own, r, sc, lse, r.live ? delta : 0.f);
@@ -1489,8 +1500,8 @@ struct Launch {
   static hipError_t bwd(const FormArgs& a, hipStream_t s) {
     const int rows = a.n * (a.nh / a.nkv);
     const size_t heads = (size_t)a.B * a.nkv;
-    if constexpr (sizeof(T) == 2 && D == 64)
-      if (a.S <= ONE && rows <= ONE) return launch<k_forms_bwd_one<T, D, CAP, SLOPES>>(256, heads, BwdOne<T, D>::LDS, a, s);
+    if (a.S <= BwdOne<T, D>::MOST && rows <= BwdOne<T, D>::MOST)
+      return launch<k_forms_bwd_one<T, D, CAP, SLOPES>>(256, heads, BwdOne<T, D>::LDS, a, s);
     const RowMode mode = row_mode(WIDE, D, heads, rows);
     hipError_t e;
     if (mode == ROWS_FEW) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, true, 4>>(256, heads * tiles(rows, 32), BwdQ<T, D, true, 4>::LDS, a, s);

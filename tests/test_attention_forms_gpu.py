@@ -90,6 +90,15 @@ def test_short_sequences(shape, form):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("form", range(len(FORMS)))
+@pytest.mark.parametrize("shape", [(3, 40, 60, 3, 3, 120), (2, 30, 50, 4, 2, 128), (2, 33, 64, 2, 2, 48), (2, 64, 64, 1, 1, 128), (2, 120, 128, 2, 2, 128),
+                                   (2, 20, 100, 10, 2, 80)], ids=lambda s: "x".join(map(str, s)))
+def test_short_sequences_of_each_width(shape, form, dtype):
+    import torch
+    _case(torch, getattr(torch, dtype), *shape, **FORMS[form], seed=4)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("w", [32, 128])
 def test_one_key_has_no_score_gradient(w, dtype):
     import torch
