@@ -233,7 +233,9 @@ __global__ void __launch_bounds__(MAX_THREADS) k_rotary_rows(RotaryArgs a, RowsP
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) ss = fmaf(v[i], v[i], ss);
-        r = 1.f / sqrtf(fmaf(row_sum(ss, pl.lg), inv_w, a.eps));
+        // (0 past the last token: rows of zeros have no norm where eps is 0)
+        const float square = fmaf(row_sum(ss, pl.lg), inv_w, a.eps);
+        r = tok < tokens ? 1.f / sqrtf(square) : 0.f;
       }
       const raw_t src = BWD ? dy[u] : x[u];
       raw_t osrc;

@@ -236,3 +236,32 @@ def test_from_the_projection_through_the_attention_and_back(heads, dtype):
         torch.cuda.synchronize()
         for name, t in eager.items():
             assert torch.equal(t, got[name]), name
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("per_head", [False, True])
+@pytest.mark.parametrize("shape", [(1, 1, 2, 1, 64), (1, 7, 3, 2, 64), (3, 5, 4, 4, 128), (1, 4099, 12, 4, 64), (2, 3, 2, 2, 33)], ids=lambda s: "x".join(map(str, s)))
+def test_norm_without_eps(shape, per_head, dtype):
+    """eps = 0 is allowed; what a workgroup works on behind the last token, rows of zeros whose norm is none, adds nothing to the gains'
+    gradients.  The bounds are those of test_head_norm_rotary_and_gradients."""
+    import torch
+    dt = getattr(torch, dtype)
+    B, S, hq, hk, w = shape
+    q, k, rand = _inputs(torch, dt, B, S, hq, hk, w, 3)
+    gains = [1 + 0.3 * rand(*((h, w) if per_head else (w,))) for h in (hq, hk)]
+    grads = [rand(*x.shape).to(dt) for x in (q, k)]
+    f = binding.rotary_form(32)
+    got = binding.mslt_head_norm_rotary(q, k, *gains, 0.0, f)
+    d = binding.mslt_head_norm_rotary_backward(q, k, *gains, 0.0, f, *grads)
+    for i, (x, gain, dy, what) in enumerate(zip((q, k), gains, grads, "qk")):
+        x, gain = x.double(), gain.double()
+        rstd = x.pow(2).mean(-1, keepdim=True).rsqrt()
+        z = x * rstd * gain
+        _close(got[i], R.rotary(z, None, 32), 2 * _pair_size(z, 32, False), 16, dt == torch.bfloat16, "y" + what)
+        dz = R.rotary(dy, None, 32, inverse=True)
+        size, dims = 2 * _pair_size(dy, 32, False), (0, 1) if per_head else (0, 1, 2)
+        off = (d["dgain_" + what].double() - (dz * x * rstd).sum(dims)).abs()
+        assert (off <= 2.0 ** -24 * 40 * (size * (x * rstd).abs()).sum(dims)).all(), f"dgain_{what}: {off.max().item():.3e}"
+        want = rstd * (dz * gain - x * rstd ** 2 * (dz * gain * x).mean(-1, keepdim=True))
+        mag = rstd * (size * gain.abs() + x.abs() * rstd ** 2 * (size * gain.abs() * x.abs()).mean(-1, keepdim=True))
+        _close(d["d" + what], want, mag, 32, dt == torch.bfloat16, "d" + what)
