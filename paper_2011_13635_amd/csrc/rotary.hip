@@ -183,7 +183,8 @@ __global__ void __launch_bounds__(MAX_THREADS) k_rotary_rows(RotaryArgs a, RowsP
   T* const yb = reinterpret_cast<T*>(const_cast<void*>(out.p)) + (long long)hh * out.sh + c * CH;
   // half layout: the piece with the other element of each pair
   const int half = a.pairs / CH;
-  const bool turned = INTER ? c * CH < 2 * a.pairs : c < 2 * half, second = !INTER && c >= half;
+  // (the table holds the tokens abreast: not so the lanes that only fill the last wavefront)
+  const bool turned = sub < pl.abreast && (INTER ? c * CH < 2 * a.pairs : c < 2 * half), second = !INTER && c >= half;
   const int other = turned && !INTER ? lane + (second ? -half : half) : lane;
   const int trig = INTER ? c * (CH / 2) : (second ? c - half : c) * CH;
   const float sign = (a.inverse != 0) != BWD ? -1.f : 1.f;

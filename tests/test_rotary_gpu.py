@@ -265,3 +265,16 @@ def test_norm_without_eps(shape, per_head, dtype):
         want = rstd * (dz * gain - x * rstd ** 2 * (dz * gain * x).mean(-1, keepdim=True))
         mag = rstd * (size * gain.abs() + x.abs() * rstd ** 2 * (size * gain.abs() * x.abs()).mean(-1, keepdim=True))
         _close(d["d" + what], want, mag, 32, dt == torch.bfloat16, "d" + what)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("heads", [(2, 1), (3, 2), (5, 2), (11, 0)])
+def test_workgroups_that_no_whole_wavefronts_fill(heads, interleaved, dtype):
+    """3, 5, 7 and 11 heads of 64 leave lanes of a workgroup's last wavefront without a token: these look nothing up."""
+    import torch
+    dt, (hq, hk) = getattr(torch, dtype), heads
+    q, k, rand = _inputs(torch, dt, 2, 83, hq, max(hk, 1), 64, 5)
+    f = binding.rotary_form(64, interleaved=interleaved)
+    for x, y in zip((q, k), binding.mslt_rotary(q, k if hk else None, f)[:2 if hk else 1]):
+        _close(y, R.rotary(x, None, 64, interleaved=interleaved), 2 * _pair_size(x, 64, interleaved), 8, dt == torch.bfloat16, "y")
