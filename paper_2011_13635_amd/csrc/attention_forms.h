@@ -217,7 +217,8 @@ __device__ __forceinline__ void add_outer(f32x16_t (&acc)[D / 32], uint32_t tile
 }
 // What rounding to bf16 took off, for a second product.  The roundings of a row's terms average out over many keys; over few, and
 // with terms that cancel, the gradient would be off by more than its own rounding.  Sequences of up to 32 keys, whose time is that of
-// a launch, take it along (1x32x4 heads of 64, backward: 7.1 -> 7.5 us; 2x4 keys, dQ: 2.5e-3 -> 1.6e-3 off, its own rounding).
+// a launch, take it along (1x32x4 heads of 64, backward: 7.1 -> 7.5 us; 2x4 keys, dQ: 2.5e-3 -> 1.6e-3 off, its own rounding), in
+// batches of any size: which kernels may take up to FINE keys have it (SHORT).
 constexpr int FINE = 32;
 __device__ __forceinline__ f32x16_t lost(const f32x16_t& p) {
   f32x16_t r;
@@ -981,7 +982,7 @@ __device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, 
     add_outer<T, D>(dq, keys, row0, dp, ln);
   }
 }
-template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW>
+template <typename T, int D, bool CAP, bool SLOPES, bool FEW, int NW, bool SHORT>
 __global__ void __launch_bounds__(64 * NW, (BwdQ<T, D, FEW, NW>::WAVES)) k_forms_bwd_q(FormArgs a) {
   fetch_args(a);
   using Q = BwdQ<T, D, FEW, NW>;
@@ -1053,7 +1054,7 @@ __global__ void __launch_bounds__(64 * NW, (BwdQ<T, D, FEW, NW>::WAVES)) k_forms
 #pragma unroll Q::SPARE ? 1 : NK
       for (int kb = 0; kb < NK; ++kb) {
         const int row0 = 32 * (FEW ? wave : kb);
-        query_block<T, D, CAP, SLOPES, MEND, Q::SPARE, FEW>(a, sc, r, kv.keys(i), kv.values(i), row0, kv.ids(i) + row0, k0 + row0, ws.lim_lo, state == 1, qf, gf,
+        query_block<T, D, CAP, SLOPES, MEND, Q::SPARE, SHORT>(a, sc, r, kv.keys(i), kv.values(i), row0, kv.ids(i) + row0, k0 + row0, ws.lim_lo, state == 1, qf, gf,
                                                        lds_addr(Gs) + row_blk * 32 * Tile<T, D>::ROWB, ln, half, l2, delta, dq, pk, rest);
       }
     }
@@ -1504,9 +1505,12 @@ struct Launch {
       return launch<k_forms_bwd_one<T, D, CAP, SLOPES>>(256, heads, BwdOne<T, D>::LDS, a, s);
     const RowMode mode = row_mode(WIDE, D, heads, rows);
     hipError_t e;
-    if (mode == ROWS_FEW) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, true, 4>>(256, heads * tiles(rows, 32), BwdQ<T, D, true, 4>::LDS, a, s);
-    else if (mode == ROWS_EIGHT) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, NW>>(64 * NW, heads * tiles(rows, 32 * NW), BwdQ<T, D, false, NW>::LDS, a, s);
-    else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
+    // (the lost parts of up to FINE keys in instances of their own where rows are not few: elsewhere they would cost registers)
+    constexpr bool PARTS = sizeof(T) == 2;
+    if (mode == ROWS_FEW) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, true, 4, PARTS>>(256, heads * tiles(rows, 32), BwdQ<T, D, true, 4>::LDS, a, s);
+    else if (PARTS && a.S <= FINE) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4, PARTS>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
+    else if (mode == ROWS_EIGHT) e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, NW, false>>(64 * NW, heads * tiles(rows, 32 * NW), BwdQ<T, D, false, NW>::LDS, a, s);
+    else e = launch<k_forms_bwd_q<T, D, CAP, SLOPES, false, 4, false>>(256, heads * tiles(rows, 128), BwdQ<T, D, false, 4>::LDS, a, s);
     if (e != hipSuccess) return e;
     if (few_keys(D, heads, a.S))
       e = launch<k_forms_bwd_kv<T, D, CAP, SLOPES, 1, 4>>(256, heads * tiles(a.S, 32) * a.row_splits, BwdKv<T, D, 1, 4>::LDS, a, s);

@@ -33,7 +33,8 @@ RowMode row_mode(bool wide, int w, size_t heads, int rows) {
 }
 // The key side at width 128 can split the rows instead (form_row_splits): 128 workgroups of 128 keys, 4x512x8 heads: 75 us against
 // 89 with 32 keys each, 1x4096 over 4: 664 against 872; but 64 workgroups, 1x1024x8 heads: 80 against 70.
-bool few_keys(int w, size_t heads, int keys) { return heads * (((size_t)keys + 127) / 128) < (w <= 64 ? 512u : 96u); }
+// Up to 32 keys there is no more than one block of 32, whatever the batch, and four wavefronts share its rows.
+bool few_keys(int w, size_t heads, int keys) { return keys <= FINE || heads * (((size_t)keys + 127) / 128) < (w <= 64 ? 512u : 96u); }
 }  // namespace forms
 
 // The keys are split where even 32 rows a workgroup come to fewer than 256 workgroups, as far as every part keeps two tiles.

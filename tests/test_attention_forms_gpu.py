@@ -336,3 +336,24 @@ def test_gradients_against_differences():
             lo[i].view(-1)[e] -= step
             slope = ((loss(*hi) - loss(*lo)) / (2 * step)).item()
             assert abs(d[name].reshape(-1)[e].item() - slope) < 2.0 ** -16, (name, e)
+
+
+@pytest.mark.parametrize("shape", [(64, 32, 32, 32, 4, 64), (64, 32, 32, 64, 8, 64), (24, 32, 32, 32, 4, 128), (64, 32, 32, 32, 4, 128), (130, 9, 30, 64, 4, 80)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("form", [{}, {"causal": True, "cap": 10.0}, {"slopes": 0.1}])
+def test_few_keys_round_gradients_once_in_any_batch(shape, form):
+    # More than 128 rows to a kv head, from batches that leave compute units idle to ones that fill the chip: the bounds of
+    # test_few_keys_round_gradients_once, which hold whatever the batch.
+    import torch
+    B, n, S, h, kv, w = shape
+    g = torch.Generator(device="cuda").manual_seed(6)
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((B, n, h, w), (B, S, kv, w), (B, S, kv, w), (B, n, h, w)))
+    slopes = torch.full((h,), form["slopes"], device="cuda") if "slopes" in form else None
+    f = {name: x for name, x in form.items() if name != "slopes"}
+    a = binding.mslt_attention(q, k, v, binding.attention_form(**f), slopes=slopes)
+    d = binding.mslt_attention_backward(q, k, v, a["out"], a["lse"], go, binding.attention_form(**f), slopes=slopes)
+    want, _ = R.attention(q, k, v, grad=go, slopes=slopes, **f)
+    for name in ("dq", "dk", "dv"):
+        value, f32, b16 = want[name]
+        own = 2.0 ** -8 * value.abs()
+        R.check(d[name], (value, f32, (b16 - own) * 2.0 ** -7 + own), True, name)
