@@ -422,13 +422,17 @@ struct Source {
     // out load the compiler does not see to that
     asm volatile("s_nop 4" : "+s"(rsrc));
   }
-  // 16 (4) bytes a lane from its offset to LDS address `to` + 16 (4) * lane; `to` the same for the wavefront
+  // 16 (4) bytes a lane from its offset to LDS address `to` + 16 (4) * lane; `to` the same for the wavefront.  The compiler has M0 to
+  // itself and warns when it is named; named it has to be, as it may set M0 once for several uses of its own.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   __device__ __forceinline__ void load16(uint32_t off, uint32_t to) const {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(off), "s"(rsrc) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(off), "s"(rsrc) : "memory", "m0");
   }
   __device__ __forceinline__ void load4(uint32_t off, uint32_t to) const {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(off), "s"(rsrc) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(off), "s"(rsrc) : "memory", "m0");
   }
+#pragma clang diagnostic pop
 };
 template <typename T, int D, int ROWS, int NW>
 struct Loader {
