@@ -226,6 +226,16 @@ def _refusal(message):
     return MsltError(MSLT_ERR_ARG, message)
 
 
+def _needed(name, form, kind, **operands):
+    """What a call cannot do without."""
+    import torch
+    if not isinstance(form, kind):
+        raise _refusal(f"{name}: form must be a {kind.__name__}, not {type(form).__name__}")
+    for what, t in operands.items():
+        if not isinstance(t, torch.Tensor):
+            raise _refusal(f"{name}: {what} must be a tensor, not {type(t).__name__}")
+
+
 def _place(name, stream, first, *others):
     """Where a call runs: the device of its first tensor and that device's current stream.  Returns the stream's handle, or None
     with a context to call again in: `stream` is another one, or the device is not the current one.  Inside the context,
@@ -329,6 +339,7 @@ def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None,
     for the results, q and k themselves allowed.  Returns them.  Enqueues only."""
     import torch
     name = "mslt_rotary"
+    _needed(name, form, RotaryForm, q=q)
     oq, ok = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, positions, oq, ok)
     if place is not None:
@@ -359,6 +370,7 @@ def mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form: RotaryForm, positions
     the two results.  Enqueues only."""
     import torch
     name = "mslt_head_norm_rotary"
+    _needed(name, form, RotaryForm, q=q, k=k, gain_q=gain_q, gain_k=gain_k)
     oq, ok = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, gain_q, gain_k, positions, oq, ok)
     if place is not None:
@@ -379,6 +391,7 @@ def mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form: RotaryForm, 
     dq and dk, grad_q and grad_k themselves allowed.  Returns a dict of dq, dk, dgain_q, dgain_k.  Enqueues only."""
     import torch
     name, lib = "mslt_head_norm_rotary_backward", load_library()
+    _needed(name, form, RotaryForm, q=q, k=k, gain_q=gain_q, gain_k=gain_k, grad_q=grad_q, grad_k=grad_k)
     dq, dk = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, gain_q, gain_k, grad_q, grad_k, positions, dq, dk)
     if place is not None:
@@ -431,6 +444,7 @@ def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, sl
     slopes: fp32 [heads].  out: tensor for the result.  Returns a dict of out and lse.  Enqueues only."""
     import torch
     name, lib = "mslt_attention", load_library()
+    _needed(name, form, AttentionForm, q=q, k=k, v=v)
     st, place = _place(name, stream, q, k, v, documents, prefix, slopes, out)
     if place is not None:
         with place:
@@ -449,6 +463,7 @@ def mslt_attention_backward(q, k, v, out, lse, grad_out, form: AttentionForm, do
     and dv.  Returns a dict of dq, dk, dv.  Enqueues only."""
     import torch
     name, lib = "mslt_attention_backward", load_library()
+    _needed(name, form, AttentionForm, q=q, k=k, v=v, out=out, lse=lse, grad_out=grad_out)
     dq, dk, dv = _given(name, "grads", grads, 3)
     st, place = _place(name, stream, q, k, v, out, lse, grad_out, documents, prefix, slopes, dq, dk, dv)
     if place is not None:
