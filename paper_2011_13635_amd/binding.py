@@ -221,19 +221,25 @@ def mslt_debug_attention(qkv, attn_mask, n_heads, head_width, mask_bias=-10000.0
     return out
 
 
-# -- operators between a layer's QKV projection and its output projection
+# -- operators between a layer's QKV projection and its output projection.  Outside torch's autograd: each has its gradient as a call of its
+#    own, and operands that require one are refused unless gradients are off (inside an autograd.Function's forward they are).
 def _refusal(message):
     return MsltError(MSLT_ERR_ARG, message)
 
 
 def _needed(name, form, kind, **operands):
-    """What a call cannot do without."""
+    """What a call cannot do without, and what it must not leave out in silence: results carry no graph, so a gradient that torch was
+    to find through them would be missing from the sum."""
     import torch
+    recording = torch.is_grad_enabled()
     if not isinstance(form, kind):
         raise _refusal(f"{name}: form must be a {kind.__name__}, not {type(form).__name__}")
     for what, t in operands.items():
         if not isinstance(t, torch.Tensor):
             raise _refusal(f"{name}: {what} must be a tensor, not {type(t).__name__}")
+        if recording and t.requires_grad:
+            raise _refusal(f"{name}: {what} requires a gradient, which torch does not find through this call: detach it or call under "
+                           "torch.no_grad(), and use the operator's own gradient")
 
 
 def _place(name, stream, first, *others):
@@ -339,7 +345,7 @@ def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None,
     for the results, q and k themselves allowed.  Returns them.  Enqueues only."""
     import torch
     name = "mslt_rotary"
-    _needed(name, form, RotaryForm, q=q)
+    _needed(name, form, RotaryForm, q=q, k=q if k is None else k)
     oq, ok = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, positions, oq, ok)
     if place is not None:
@@ -444,7 +450,7 @@ def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, sl
     slopes: fp32 [heads].  out: tensor for the result.  Returns a dict of out and lse.  Enqueues only."""
     import torch
     name, lib = "mslt_attention", load_library()
-    _needed(name, form, AttentionForm, q=q, k=k, v=v)
+    _needed(name, form, AttentionForm, q=q, k=k, v=v, slopes=q if slopes is None else slopes)
     st, place = _place(name, stream, q, k, v, documents, prefix, slopes, out)
     if place is not None:
         with place:
@@ -463,7 +469,7 @@ def mslt_attention_backward(q, k, v, out, lse, grad_out, form: AttentionForm, do
     and dv.  Returns a dict of dq, dk, dv.  Enqueues only."""
     import torch
     name, lib = "mslt_attention_backward", load_library()
-    _needed(name, form, AttentionForm, q=q, k=k, v=v, out=out, lse=lse, grad_out=grad_out)
+    _needed(name, form, AttentionForm, q=q, k=k, v=v, out=out, lse=lse, grad_out=grad_out, slopes=q if slopes is None else slopes)
     dq, dk, dv = _given(name, "grads", grads, 3)
     st, place = _place(name, stream, q, k, v, out, lse, grad_out, documents, prefix, slopes, dq, dk, dv)
     if place is not None:

@@ -357,3 +357,31 @@ def test_few_keys_round_gradients_once_in_any_batch(shape, form):
         value, f32, b16 = want[name]
         own = 2.0 ** -8 * value.abs()
         R.check(d[name], (value, f32, (b16 - own) * 2.0 ** -7 + own), True, name)
+
+
+def test_as_part_of_a_torch_graph():
+    """Wrapped into an autograd.Function, whose forward and backward run with gradients off; leaves are refused outside of one."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(12)
+    leaves = [torch.randn(s, generator=g, device="cuda", requires_grad=True) for s in ((2, 50, 4, 32), (2, 50, 2, 32), (2, 50, 2, 32))]
+    form = binding.attention_form(causal=True)
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v):
+            f = binding.mslt_attention(q, k, v, form)
+            ctx.save_for_backward(q, k, v, f["out"], f["lse"])
+            return f["out"]
+
+        @staticmethod
+        def backward(ctx, grad):
+            d = binding.mslt_attention_backward(*ctx.saved_tensors, grad.contiguous(), form)
+            return d["dq"], d["dk"], d["dv"]
+
+    go = torch.randn(leaves[0].shape, generator=g, device="cuda")
+    (Attention.apply(*leaves) * go).sum().backward()
+    want, _ = R.attention(*(x.detach() for x in leaves), causal=True, grad=go)
+    for x, name in zip(leaves, ("dq", "dk", "dv")):
+        R.check(x.grad, want[name], False, name)
+    with pytest.raises(binding.MsltError, match="requires a gradient"):
+        binding.mslt_attention(*leaves, form)
