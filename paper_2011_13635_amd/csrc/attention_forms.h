@@ -500,10 +500,6 @@ __device__ __forceinline__ int key_limit(const FormArgs& a, int pos, int prefix)
   return a.causal ? min(a.S, max(pos + 1, prefix)) : a.S;
 }
 
-// Factor of the gradients of queries and keys.  The softmax of a single score is one whatever the score: they are zero, where the
-// roundings of dp and delta would leave something.
-__device__ __forceinline__ float score_gradient(const FormArgs& a) { return a.S > 1 ? a.scale : 0.f; }
-
 // What a lane that owns a query row knows of it.
 struct RowOf {
   int R, qi, head, pos, id, lim;
@@ -525,6 +521,13 @@ __device__ __forceinline__ RowOf row_of(const FormArgs& a, int R, int b, int hk,
   r.slope = a.slopes ? a.slopes[r.head] * (a.cap > 0.f ? LOG2E : 1.f / a.scale) : 0.f;
   return r;
 }
+// Factors of the gradients of queries and keys.  The softmax of a single score is one whatever the score, its gradient zero.  So it is
+// exactly where the position leaves a row one key (causal: the first row), and for the keys where there is one in all.  Where it is
+// documents that leave a row one key, the roundings of dp and delta remain, as they do in every row: fp32's, and in bf16 2^-16 of
+// the size of dO O, as delta is mended.
+__device__ __forceinline__ float query_gradient(const FormArgs& a, const RowOf& r) { return r.lim > 1 ? a.scale : 0.f; }
+__device__ __forceinline__ float key_gradient(const FormArgs& a) { return a.S > 1 ? a.scale : 0.f; }
+
 // Limits and document entries of the live rows among R0 .. R0 + count - 1.  Limits grow with the position: the first and the last
 // row inside the tensor bound them.
 struct Span {
@@ -1086,7 +1089,7 @@ __global__ void __launch_bounds__(64 * NW, (BwdQ<T, D, FEW, NW>::WAVES)) k_forms
   }
   if (!r.in) return;
   if (half == 0) a.delta[lrow] = delta;
-  store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, score_gradient(a), r.live);
+  store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, query_gradient(a, r), r.live);
 }
 
 // the 16 of 32 rows' values that this half-wave's registers stand for
@@ -1316,10 +1319,10 @@ __global__ void __launch_bounds__(64 * NW, (BwdKv<T, D, BLOCKS, NW>::WAVES)) k_f
   if (a.row_splits > 1) {
     const size_t all = (size_t)a.B * a.nkv * a.S, row = ((size_t)b * a.nkv + hk) * a.S + key;
     float* const out = a.part + ((size_t)split * 2 * all + row) * a.w;
-    store_row<float, D>(out, dk, half, a.w, score_gradient(a), live);
+    store_row<float, D>(out, dk, half, a.w, key_gradient(a), live);
     store_row<float, D>(out + all * a.w, dv, half, a.w, 1.f, live);
   } else {
-    store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, score_gradient(a), live);
+    store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)key * a.dk.sr, dk, half, a.w, key_gradient(a), live);
     store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)key * a.dv.sr, dv, half, a.w, 1.f, live);
   }
 }
@@ -1428,7 +1431,7 @@ __global__ void __launch_bounds__(256, (BwdOne<T, D>::WAVES)) k_forms_bwd_one(Fo
 #pragma unroll
         for (int j = 0; j < 16; ++j) dq[i][j] = fmaf(-rest, pk[i][j], dq[i][j]);
     }
-    if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, score_gradient(a), r.live);
+    if (r.in) store_row<T, D>(head_out<T>(a.dq, b, r.head) + (long long)r.qi * a.dq.sr, dq, half, a.w, query_gradient(a, r), r.live);
   }
   if (half == 0) m.template put<sizeof(T) == 2 && !CAP>(own, r, sc, lse, r.live ? delta : 0.f);
 
@@ -1458,7 +1461,7 @@ __global__ void __launch_bounds__(256, (BwdOne<T, D>::WAVES)) k_forms_bwd_one(Fo
     key_block<T, D, CAP, SLOPES, false, true>(a, sc, m, first_tile, second_tile, R0 / 32, kf, vf, 0, 0, own, kid, mask, ln, half, dk, dv);
   }
   if (!in) return;
-  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, score_gradient(a), live);
+  store_row<T, D>(head_out<T>(a.dk, b, hk) + (long long)own * a.dk.sr, dk, half, a.w, key_gradient(a), live);
   store_row<T, D>(head_out<T>(a.dv, b, hk) + (long long)own * a.dv.sr, dv, half, a.w, 1.f, live);
 }
 

@@ -385,3 +385,36 @@ def test_as_part_of_a_torch_graph():
         R.check(x.grad, want[name], False, name)
     with pytest.raises(binding.MsltError, match="requires a gradient"):
         binding.mslt_attention(*leaves, form)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(2, 90, 90, 4, 2, 64), (3, 60, 60, 2, 2, 128), (1, 400, 400, 6, 2, 64), (40, 200, 200, 8, 8, 64), (2, 3, 300, 4, 2, 128)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+def test_rows_that_see_one_key_among_many(shape, cap, dtype):
+    # The gradient of a single score is zero.  Exactly so in the first row of a causal sequence.  Documents of one token leave roundings:
+    # fp32's; in bf16 dP - delta is off by half a step of the stored output, 2^-8 of the size of dO O, of which the mended delta
+    # takes off all but what rounding that to bf16 leaves, 2^-8 of it: 2^-16, where forms_reference's b16 counts 2^-7 for delta
+    # (and twice the probability's).  Doubled for products of roundings: b16 times 2^-8.
+    import torch
+    dt = getattr(torch, dtype)
+    B, n, S, h, kv, w = shape
+    g = torch.Generator(device="cuda").manual_seed(13)
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda").mul(1.5).to(dt) for s in ((B, n, h, w), (B, S, kv, w), (B, S, kv, w), (B, n, h, w)))
+    form = binding.attention_form(cap=cap, causal=True)
+    if n == S:
+        f = binding.mslt_attention(q, k, v, form)
+        d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form)
+        assert (d["dq"][:, 0] == 0).all()
+        want, _ = R.attention(q, k, v, cap=cap, causal=True, grad=go)
+        for name in ("dq", "dk", "dv"):
+            R.check(d[name], want[name], dt == torch.bfloat16, name)
+    docs = torch.arange(S, dtype=torch.int32, device="cuda").expand(B, S).contiguous()
+    form = binding.attention_form(cap=cap)
+    f = binding.mslt_attention(q, k, v, form, documents=docs)
+    d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form, documents=docs)
+    want, _ = R.attention(q, k, v, cap=cap, documents=docs, grad=go)
+    for name in ("dq", "dk"):
+        value, f32, b16 = want[name]
+        assert (value.abs() <= f32).all()      # (zero but for float64's own roundings)
+        R.check(d[name], (value, f32, b16 * 2.0 ** -8), dt == torch.bfloat16, name)
