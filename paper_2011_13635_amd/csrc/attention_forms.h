@@ -247,10 +247,15 @@ __device__ __forceinline__ void add_outer2(f32x16_t (&x)[D / 32], f32x16_t (&y)[
 }
 
 // Score in base 2 from the product x of a query and a key, and what the gradient is multiplied by behind the cap.
-// tanh y = 1 - 2 / (1 + e^2y): absolute error a few 2^-24 for any y, and the score's is cap times that.  Where all of a lane's scores
-// lie within six tenths of the cap, y (c0 + c1 y^2 + .. + c4 y^8) is nearer and faster, six multiply-adds in place of two
-// transcendental instructions (8.4 cycles each against 3) and three more; fitted to the least largest error relative to y, 7.4e-8.
+// tanh y = 1 - 2 / (1 + e^2y): absolute error a few 2^-24 for any y, and the score's is cap times that.  Up to six tenths of the cap,
+// y (c0 + c1 y^2 + .. + c4 y^8) is nearer and faster, six multiply-adds in place of two transcendental instructions (8.4 cycles each
+// against 3) and three more; fitted to the least largest error relative to y, 7.4e-8.
 // Caps so far above the scale that c4's factor falls below the least fp32: within a twentieth, where c3 y^6 adds less than 2^-29.
+// Where a score of a wavefront's block of 32 x 32 lies beyond, each takes its own formula in fp32, so that no score loses digits to its
+// neighbours (cap 20 and scores of 6 typically: 4x1024x8 heads of 64, forward 98 -> 102 us, backward 318 -> 329).  In bf16 all take
+// the first one as long as its error, 3 2^-24 of a cap below 2^10 in base 2, stays a tenth of the half step that probabilities are
+// rounded by (1x8192x12 heads of 64: 452 us, each its own 550).
+constexpr float SHARED_CAP = 0x1p10f;
 struct Score {
   float a, c;              // no cap: s2 = a x.  cap: s2 = c tanh, exponent a x
   float p[5], reach;       // s2 = x (p0 + p1 x^2 + ...) for |x| <= reach
@@ -270,34 +275,33 @@ __device__ __forceinline__ Score make_score(float scale, float cap) {
   }
   return f;
 }
-template <bool CAP>
-__device__ __forceinline__ float score2(const Score& f, float x, float& damp) {
-  if constexpr (!CAP) return f.a * x;
-  const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f.a * x)), 1.f);
-  damp = fmaf(-t, t, 1.f);
-  return f.c * t;
+__device__ __forceinline__ float near_score(const Score& f, float x) {
+  const float u = x * x;
+  return x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, f.p[4], f.p[3]), f.p[2]), f.p[1]), f.p[0]);
 }
-// the same for 16 scores at once
-template <bool DAMP>
+__device__ __forceinline__ float far_score(const Score& f, float x) {
+  return f.c * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(f.a * x)), 1.f);
+}
+// 16 scores at once
+template <typename T, bool DAMP>
 __device__ __forceinline__ void cap_scores(const Score& f, f32x16_t& s, f32x16_t& damp) {
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(s[i]));
   if (!__any(!(top <= f.reach))) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = near_score(f, s[i]);
+  } else if (sizeof(T) == 2 && f.c < SHARED_CAP) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = far_score(f, s[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = fabsf(s[i]) <= f.reach ? near_score(f, s[i]) : far_score(f, s[i]);
+  }
+  if constexpr (DAMP) {      // 1 - tanh^2 to a few 2^-24, from the score (beside the tanh it takes registers: 375 us for 318 at 4x1024x8 heads in fp32)
     const float ic2 = 1.f / (f.c * f.c);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float u = s[i] * s[i];
-      s[i] *= fmaf(u, fmaf(u, fmaf(u, fmaf(u, f.p[4], f.p[3]), f.p[2]), f.p[1]), f.p[0]);
-      if constexpr (DAMP) damp[i] = fmaf(-ic2 * s[i], s[i], 1.f);
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float d = 1.f;
-    s[i] = score2<true>(f, s[i], d);
-    if constexpr (DAMP) damp[i] = d;
+    for (int i = 0; i < 16; ++i) damp[i] = fmaf(-ic2 * s[i], s[i], 1.f);
   }
 }
 
@@ -594,9 +598,9 @@ __device__ __forceinline__ void positions_range(const int2* r, int p0, int p1, i
 // score_factor() is the score in base 2; without a cap that leaves the factor to the exponential's own multiply-add.
 template <bool CAP>
 __device__ __forceinline__ float score_factor(const Score& f) { return CAP ? 1.f : f.a; }
-template <bool CAP, bool SLOPES, bool DAMP>
+template <typename T, bool CAP, bool SLOPES, bool DAMP>
 __device__ __forceinline__ void open_scores(const Score& f, const RowOf& r, int k0, int half, f32x16_t& s, f32x16_t& damp) {
-  if constexpr (CAP) cap_scores<DAMP>(f, s, damp);
+  if constexpr (CAP) cap_scores<T, DAMP>(f, s, damp);
   if constexpr (SLOPES) {
     const float far = (float)(r.pos - k0 - 4 * half);
 #pragma unroll
@@ -620,10 +624,10 @@ __device__ __forceinline__ void hide(const FormArgs& a, const RowOf& r, const in
     }
   }
 }
-template <bool CAP, bool SLOPES, bool DAMP>
+template <typename T, bool CAP, bool SLOPES, bool DAMP>
 __device__ __forceinline__ void scores(const FormArgs& a, const Score& f, const RowOf& r, const int* ids, int k0, int limit, int half, bool mask,
                                        f32x16_t& s, f32x16_t& damp) {
-  open_scores<CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
+  open_scores<T, CAP, SLOPES, DAMP>(f, r, k0, half, s, damp);
   if (mask) hide(a, r, ids, k0, limit, half, s);
 }
 
@@ -790,7 +794,7 @@ __global__ void __launch_bounds__(64 * NW, (Fwd<T, D, CAP, FEW, NW>::WAVES)) k_f
       for (int kb = 0; kb < NK; ++kb) {
         const int row0 = 32 * (kb0 + kb);
         f32x16_t s = dot_rows<T, D>(kv.keys(i), row0, qf, ln);
-        scores<CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, unused);
+        scores<T, CAP, SLOPES, false>(a, sc, r, kv.ids(i) + row0, k0 + row0, ws.lim_lo, half, state == 1, s, unused);
         refer(factor * row_top(s));
         powers(s);
         add_outer<T, D>(o, kv.values(i), row0, s, ln);
@@ -968,7 +972,7 @@ __device__ __forceinline__ void query_block(const FormArgs& a, const Score& sc, 
   else dp = dot_rows<T, D>(values, row0, gf, ln);
   feed<T, Tile<T, D>::NS, 1, 1>();
   feed<T, Tile<T, D>::NS, SPARE ? 2 : 1, 1>();
-  scores<CAP, SLOPES, true>(a, sc, r, ids, k0, limit, half, mask, s, damp);
+  scores<T, CAP, SLOPES, true>(a, sc, r, ids, k0, limit, half, mask, s, damp);
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     float p = __builtin_amdgcn_exp2f(fmaf(s[j], factor, -l2)), ds = p * (dp[j] - delta);
@@ -1139,7 +1143,7 @@ __device__ __forceinline__ void key_block(const FormArgs& a, const Score& sc, co
   feed<T, Tile<T, D>::NS, SPARE ? 2 : 1, 1>();
   feed<T, Tile<T, D>::NS, SPARE ? 2 : 1, 1>();
   f32x16_t damp;
-  if constexpr (CAP) cap_scores<true>(sc, s, damp);
+  if constexpr (CAP) cap_scores<T, true>(sc, s, damp);
   if constexpr (SLOPES) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {

@@ -418,3 +418,30 @@ def test_rows_that_see_one_key_among_many(shape, cap, dtype):
         value, f32, b16 = want[name]
         assert (value.abs() <= f32).all()      # (zero but for float64's own roundings)
         R.check(d[name], (value, f32, b16 * 2.0 ** -8), dt == torch.bfloat16, name)
+
+
+@pytest.mark.parametrize("dtype,cap", [("float32", 400.0), ("float32", 3000.0), ("bfloat16", 30000.0)])
+@pytest.mark.parametrize("shape", [(2, 90, 90, 2, 2, 64), (1, 64, 64, 2, 2, 128), (1, 300, 300, 4, 2, 64), (1, 3, 700, 4, 2, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_scores_near_the_cap_leave_others_their_digits(shape, cap, dtype):
+    # Every seventh query's scores reach the cap, all others are some tens at most: those may be off by what they are off without a cap
+    # (16 roundings of a score's terms, to which the polynomial adds six) and in bf16 by its own roundings; not by roundings of the cap.
+    import torch
+    dt = getattr(torch, dtype)
+    B, n, S, h, kv, w = shape
+    g = torch.Generator(device="cuda").manual_seed(14)
+    q, k, v, go = (torch.randn(s, generator=g, device="cuda").mul(1.5) for s in ((B, n, h, w), (B, S, kv, w), (B, S, kv, w), (B, n, h, w)))
+    large = torch.arange(n, device="cuda") % 7 == 1
+    q[:, large] *= cap / 3
+    go[:, large] = 0
+    q, k, v, go = (x.to(dt) for x in (q, k, v, go))
+    form = binding.attention_form(cap=cap)
+    f = binding.mslt_attention(q, k, v, form)
+    d = binding.mslt_attention_backward(q, k, v, f["out"], f["lse"], go, form)
+    want, lse = R.attention(q, k, v, cap=cap, grad=go)
+    plain = q.clone()
+    plain[:, large] = 0
+    bounds, _ = R.attention(plain, k, v, grad=go)
+    for name in ("out", "dq"):
+        R.check({**f, **d}[name][:, ~large], tuple(x[:, ~large] for x in (want[name][0], *bounds[name][1:])), dt == torch.bfloat16, name)
+    # the log-sum-exp: of scores whose terms add up to less than 2^7, 32 roundings of that
+    assert ((f["lse"].double() - lse)[:, :, ~large].abs() <= 32 * 2.0 ** -24 * 2 ** 7).all()
