@@ -227,6 +227,17 @@ def _refusal(message):
     return MsltError(MSLT_ERR_ARG, message)
 
 
+def _suspect(form, kind, *operands):
+    """Whether _needed() has to look closer: a call's fast way past it."""
+    try:
+        for t in operands:
+            if t.requires_grad:
+                return True
+    except AttributeError:
+        return True
+    return type(form) is not kind
+
+
 def _needed(name, form, kind, **operands):
     """What a call cannot do without, and what it must not leave out in silence: results carry no graph, so a gradient that torch was
     to find through them would be missing from the sum."""
@@ -345,7 +356,8 @@ def mslt_rotary(q, k, form: RotaryForm, positions=None, inverse=False, out=None,
     for the results, q and k themselves allowed.  Returns them.  Enqueues only."""
     import torch
     name = "mslt_rotary"
-    _needed(name, form, RotaryForm, q=q, k=q if k is None else k)
+    if _suspect(form, RotaryForm, q, q if k is None else k):
+        _needed(name, form, RotaryForm, q=q, k=q if k is None else k)
     oq, ok = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, positions, oq, ok)
     if place is not None:
@@ -376,7 +388,8 @@ def mslt_head_norm_rotary(q, k, gain_q, gain_k, eps, form: RotaryForm, positions
     the two results.  Enqueues only."""
     import torch
     name = "mslt_head_norm_rotary"
-    _needed(name, form, RotaryForm, q=q, k=k, gain_q=gain_q, gain_k=gain_k)
+    if _suspect(form, RotaryForm, q, k, gain_q, gain_k):
+        _needed(name, form, RotaryForm, q=q, k=k, gain_q=gain_q, gain_k=gain_k)
     oq, ok = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, gain_q, gain_k, positions, oq, ok)
     if place is not None:
@@ -397,7 +410,8 @@ def mslt_head_norm_rotary_backward(q, k, gain_q, gain_k, eps, form: RotaryForm, 
     dq and dk, grad_q and grad_k themselves allowed.  Returns a dict of dq, dk, dgain_q, dgain_k.  Enqueues only."""
     import torch
     name, lib = "mslt_head_norm_rotary_backward", load_library()
-    _needed(name, form, RotaryForm, q=q, k=k, gain_q=gain_q, gain_k=gain_k, grad_q=grad_q, grad_k=grad_k)
+    if _suspect(form, RotaryForm, q, k, gain_q, gain_k, grad_q, grad_k):
+        _needed(name, form, RotaryForm, q=q, k=k, gain_q=gain_q, gain_k=gain_k, grad_q=grad_q, grad_k=grad_k)
     dq, dk = _given(name, "out", out, 2)
     st, place = _place(name, stream, q, k, gain_q, gain_k, grad_q, grad_k, positions, dq, dk)
     if place is not None:
@@ -450,7 +464,8 @@ def mslt_attention(q, k, v, form: AttentionForm, documents=None, prefix=None, sl
     slopes: fp32 [heads].  out: tensor for the result.  Returns a dict of out and lse.  Enqueues only."""
     import torch
     name, lib = "mslt_attention", load_library()
-    _needed(name, form, AttentionForm, q=q, k=k, v=v, slopes=q if slopes is None else slopes)
+    if _suspect(form, AttentionForm, q, k, v, q if slopes is None else slopes):
+        _needed(name, form, AttentionForm, q=q, k=k, v=v, slopes=q if slopes is None else slopes)
     st, place = _place(name, stream, q, k, v, documents, prefix, slopes, out)
     if place is not None:
         with place:
@@ -469,7 +484,8 @@ def mslt_attention_backward(q, k, v, out, lse, grad_out, form: AttentionForm, do
     and dv.  Returns a dict of dq, dk, dv.  Enqueues only."""
     import torch
     name, lib = "mslt_attention_backward", load_library()
-    _needed(name, form, AttentionForm, q=q, k=k, v=v, out=out, lse=lse, grad_out=grad_out, slopes=q if slopes is None else slopes)
+    if _suspect(form, AttentionForm, q, k, v, out, lse, grad_out, q if slopes is None else slopes):
+        _needed(name, form, AttentionForm, q=q, k=k, v=v, out=out, lse=lse, grad_out=grad_out, slopes=q if slopes is None else slopes)
     dq, dk, dv = _given(name, "grads", grads, 3)
     st, place = _place(name, stream, q, k, v, out, lse, grad_out, documents, prefix, slopes, dq, dk, dv)
     if place is not None:
