@@ -312,7 +312,8 @@ typedef struct {
  * scaling 0 no; 1 f_i/factor; 2 by how often the pair turns within original_length positions, w = original_length*f_i/2pi:
  * f_i * (t + (1-t)/factor), t = (w - low_turns)/(high_turns - low_turns) held to 0..1.  Pair i is elements (i, i +
  * rotary_width/2), or (2i, 2i+1) when interleaved; elements from rotary_width on stay as they are.  The rotated elements
- * are multiplied by magnitude.  Angles are exact to 2^-32 of a turn at any position. */
+ * are multiplied by magnitude.  Angles are within 2^-25 of a turn at any position (their conversion to fp32 2^-26, the frequency's
+ * rounding the rest at the farthest). */
 typedef struct {
   int rotary_width;   /* even, 0 to the head width */
   int interleaved;
@@ -330,8 +331,9 @@ int mslt_rotary(void* hip_stream, int precision, int batch, int seq, int q_heads
                 const mslt_heads* k, const int32_t* positions, const mslt_rotary_form* form, int inverse,
                 const mslt_heads* q_out, const mslt_heads* k_out);
 
-/* The same rotation of x * gain / sqrt(mean(x^2) + eps), the mean over each head.  gain_q, gain_k: fp32 [width], or
- * [heads, width] with gain_per_head != 0. */
+/* The same rotation of x * gain / sqrt(mean(x^2) + eps), the mean over each head, whose squares have to add up within fp32; eps
+ * 0 or above (0: no head may be all zeros).  Queries and keys both.  gain_q, gain_k: fp32 [width], or [heads, width] with
+ * gain_per_head != 0. */
 int mslt_head_norm_rotary(void* hip_stream, int precision, int batch, int seq, int q_heads, int k_heads, int width,
                           const mslt_heads* q, const mslt_heads* k, const float* gain_q, const float* gain_k, int gain_per_head,
                           float eps, const int32_t* positions, const mslt_rotary_form* form, const mslt_heads* q_out,
@@ -352,7 +354,10 @@ int mslt_head_norm_workspace(int batch, int seq, int q_heads, int k_heads, int w
  * document only (the same entry of documents, not negative), and with causal != 0 only keys at its position or before, or
  * among the first prefix[b] of its sequence.  A query that sees no key gets zeros, a log-sum-exp of -infinity, and no
  * gradient.  Rows of a negative document (padding) may hold anything, NaN included: none of it is used, their outputs and
- * gradients are zeros.  All other rows must be finite, and scores within 1e30. */
+ * gradients are zeros.  All other rows must be finite, those that a mask hides from some queries included, and scores within
+ * 1e30.  There is no dropout.  Sums, scores and the log-sum-exp are fp32; with bf16 operands probabilities and score gradients
+ * are rounded to bf16 once on their way into the products with values, keys, queries and output gradients (gradients of up to 32
+ * keys: in two parts), and under a cap below 710 a score may be off by 3 2^-24 of the cap. */
 typedef struct {
   float scale;              /* 2^-20 to 2^20 */
   float cap;                /* 0: none; else scale / cap 2^-24 to 2^12 */
@@ -367,7 +372,10 @@ typedef struct {
  * multiples of 16 bytes; the rows of k and v at most 2^22 elements apart (backward: those of q and grad_out too, and the
  * heads of a group within 2^28 elements).  keys at most 2^24, batch * heads 2^20, batch * heads * queries 2^30,
  * batch * kv_heads * keys 2^29.  lse: fp32 [batch, heads, queries], natural log-sum-exp of the scores.  workspace: DEVICE scratch, 16-byte aligned, of
- * the bytes that mslt_attention_workspace reports for the direction. */
+ * the bytes that mslt_attention_workspace reports for the direction: 4 a row of every head (backward) and 8 for 64 positions of
+ * a sequence, and where a batch leaves compute units idle fp32 sums of parts, forward batch * heads * queries * width * 4 for
+ * each part of the keys, backward batch * kv_heads * keys * width * 8 for each part of the rows (1 x 8192
+ * keys, 16 heads of 128 over 4: 135 MB; from 4 such sequences on 2 MB). */
 int mslt_attention(void* hip_stream, int precision, int batch, int queries, int keys, int heads, int kv_heads, int width,
                    const mslt_heads* q, const mslt_heads* k, const mslt_heads* v, const mslt_attention_form* form,
                    const mslt_heads* out, float* lse, void* workspace, size_t workspace_bytes);

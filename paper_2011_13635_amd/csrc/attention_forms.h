@@ -175,7 +175,10 @@ __device__ __forceinline__ bf16x8_t frag_transposed(uint32_t tile, int row0, int
 }
 // acc[d, lane's column] += sum over 32 tile rows from row0 of tile[row][d] * p[row, column].  bf16: p is rounded to bf16
 // here, the one rounding between the two products (the sum of a row is taken before it); a term is then off by half a step,
-// 2^-8 of itself, as the operands of the first product already are.
+// 2^-8 of itself, as the operands of the first product already are.  Results are off by 2.0e-3 to 2.4e-3 (root of the mean square,
+// listed training shapes), of which their own rounding alone is 1.66e-3.  A second part of what is rounded off, as lost() gives it, takes
+// them to 1.66e-3 and costs up to a quarter: forward 1x8192x12 heads of 64 390 -> 474 us, 1x8192x16 of 128 353 -> 442, 64x128x16 18.6 -> 21.2;
+// backward 1300 -> 1570, 32x512x16 218 -> 251, 64x128x16 45 -> 47.  Callers that need it have fp32 operands.
 template <int D>
 __device__ __forceinline__ void add_packed(f32x16_t (&acc)[D / 32], uint32_t tile, int row0, const bf16x8_t (&f)[2], const Lane<bf16, D>& l) {
 #pragma unroll
@@ -949,7 +952,9 @@ __device__ __forceinline__ float dot_chunk(u32x4_t x, u32x4_t y) {
 // bf16: the stored output is rounded, so sum_d dO O is not quite the delta that makes a row of p (dp - delta) add up to zero, and
 // in rows that look at few keys what is left is of the gradient's own size.  The kernel finds it, rest = sum p (dp - delta),
 // and takes it out: delta grows by rest, dQ loses rest * sum p damp k, for which those sums are formed beside dQ.
-// bf16 at width 128: the registers of dQ, of those sums and of the queries leave no room for dO's, which stay in LDS (SPARE).
+// bf16 at width 128: the registers of dQ, of those sums and of the queries leave no room for dO's, which stay in LDS (SPARE).  Eight
+// wavefronts, two to a SIMD, still spill 5 with a bias and, in the tile loop too, 31 to 33 with a cap; four, one to a SIMD, spill none
+// and are slower (cap 20, both sides: 1x8192x16 heads over 4 1458 us against 1597, 32x512x16 534 against 608).
 // FEW as in the forward.
 template <typename T, int D, bool FEW, int NW>
 struct BwdQ {
@@ -1194,8 +1199,8 @@ __device__ __forceinline__ void key_block(const FormArgs& a, const Score& sc, co
 template <typename T, int D, int BLOCKS, int NW>
 struct BwdKv {
   static constexpr int PARTS = NW / BLOCKS, RT = PARTS == 4 ? 128 : 64, TILE = RT * Tile<T, D>::ROWB, STAGE = 2 * TILE;
-  // Wavefronts that share a SIMD (fp32 at width 64 spills a few registers for it and has one stage: 4x1024x8 heads, both sides, 369 us
-  // with one, 322 with two; 3x203x12, a workgroup to each compute unit, 36 and 37).
+  // Wavefronts that share a SIMD.  fp32 at width 64 has one stage for it and spills 9 to 21 vector registers, with a cap 26 to 49, and 38 to
+  // 60 scalar ones (4x1024x8 heads, both sides, 369 us with one, 322 with two; 3x203x12, a workgroup to each compute unit, 36 and 37).
   static constexpr int WAVES = D == 64 || NW == 8 ? 2 : 1, BUFS = TILE > (NW == 4 && WAVES == 2 ? 32767 : 32768) ? 1 : 2;
   static constexpr bool SPARE = NW == 8;
   static constexpr int LDS = BUFS * STAGE + (SPARE ? 2 * 128 * Tile<T, D>::ROWB : 0);
