@@ -338,7 +338,8 @@ def test_gradients_against_differences():
             assert abs(d[name].reshape(-1)[e].item() - slope) < 2.0 ** -16, (name, e)
 
 
-@pytest.mark.parametrize("shape", [(64, 32, 32, 32, 4, 64), (64, 32, 32, 64, 8, 64), (24, 32, 32, 32, 4, 128), (64, 32, 32, 32, 4, 128), (130, 9, 30, 64, 4, 80)],
+@pytest.mark.parametrize("shape", [(64, 32, 32, 32, 4, 64), (64, 32, 32, 64, 8, 64), (24, 32, 32, 32, 4, 128), (64, 32, 32, 32, 4, 128), (130, 9, 30, 64, 4, 80),
+                                   (2, 32, 32, 64, 1, 64)],
                          ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("form", [{}, {"causal": True, "cap": 10.0}, {"slopes": 0.1}])
 def test_few_keys_round_gradients_once_in_any_batch(shape, form):
